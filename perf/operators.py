@@ -163,7 +163,8 @@ def _run_own(s):
             y, z8 = ops.linear(s["x"], s["w"], s["bias"]), None
         else:
             y, z8 = ops.linear(s["x"], s["w"], s["bias"], act=c["act"], save="z8")
-        return (y,) + tuple(ops.linear_backward(s["dy"], x8, s["w"], z=z8, act=c["act"]))
+        return (y,) + tuple(ops.linear_backward(s["dy"], x8, s["w"], z=z8, act=c["act"],
+                                                 bias_dtype=s["bias"].dtype))
     if op == "layer_norm":
         return ops.layer_norm(s["x"], s["weight"], s["bias"], eps=EPS, save=c["save"])
     if op == "layer_norm_backward":
