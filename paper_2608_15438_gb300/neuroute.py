@@ -27,7 +27,10 @@ EXPORTS = ["nr_status_string", "nr_params_default", "nr_index_load", "nr_index_f
            "nr_centroid_dists", "nr_build_begin", "nr_build_encode", "nr_build_set_logits",
            "nr_build_finish", "nr_build_place", "nr_build_end", "nr_build_free",
            "nr_measure_gather", "nr_measure_read", "nr_bucket_scores", "nr_calib_observe", "nr_calib_fit_s_max",
-           "nr_calib_fit_gate", "nr_calibrate"]
+           "nr_calib_fit_gate", "nr_calibrate",
+           "nr_linear_forward_workspace", "nr_linear_backward_workspace", "nr_linear_forward",
+           "nr_linear_backward", "nr_layer_norm_backward_workspace", "nr_layer_norm_forward",
+           "nr_layer_norm_backward", "nr_checkpoint8_write", "nr_checkpoint8_read", "nr_ops_status"]
 
 
 class NRError(RuntimeError):
@@ -105,9 +108,22 @@ def lib():
         L.nr_build_end.argtypes = [vp, ctypes.POINTER(vp)]
         L.nr_build_free.argtypes = [vp]
         L.nr_build_free.restype = None
+        # the encoder operators (neuroute_ops.h); their structures come packed in bytes
+        sz, cb = ("nr_linear_forward_workspace", "nr_linear_backward_workspace",
+                  "nr_layer_norm_backward_workspace"), ctypes.c_char_p
+        for name in sz:
+            getattr(L, name).argtypes = [cb, i32]
+            getattr(L, name).restype = i64
+        L.nr_linear_forward.argtypes = [cb, i32, vp, i64, vp]
+        L.nr_linear_backward.argtypes = [cb, i32, vp, i64, vp]
+        L.nr_layer_norm_forward.argtypes = [cb, i32, vp]
+        L.nr_layer_norm_backward.argtypes = [cb, i32, vp, i64, vp]
+        L.nr_checkpoint8_write.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp]
+        L.nr_checkpoint8_read.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, i32, vp]
+        L.nr_ops_status.argtypes = [i32]
         for name in EXPORTS:
             if name not in ("nr_status_string", "nr_index_free", "nr_kernel_launches",
-                            "nr_build_free"):
+                            "nr_build_free") + sz:
                 getattr(L, name).restype = i32
         _LIB = L
     return _LIB
