@@ -147,6 +147,11 @@ nr_status nr_checkpoint8_read(const void *codes, const void *scales, int64_t m, 
  * (their outputs are then undefined), else NR_OK. */
 nr_status nr_ops_status(int device);
 
+/* Execution only: the limit of the bounded waits, in microseconds, for calls
+ * that follow. 0 (default): 1 s. < 0: a wait whose phase is not complete when
+ * first tested expires at once, which exercises the failure path. */
+nr_status nr_ops_wait_limit(int64_t us);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,8 @@ EXPORTS = ["nr_status_string", "nr_params_default", "nr_index_load", "nr_index_f
            "nr_calib_fit_gate", "nr_calibrate",
            "nr_linear_forward_workspace", "nr_linear_backward_workspace", "nr_linear_forward",
            "nr_linear_backward", "nr_layer_norm_backward_workspace", "nr_layer_norm_forward",
-           "nr_layer_norm_backward", "nr_checkpoint8_write", "nr_checkpoint8_read", "nr_ops_status"]
+           "nr_layer_norm_backward", "nr_checkpoint8_write", "nr_checkpoint8_read", "nr_ops_status",
+           "nr_ops_wait_limit"]
 
 
 class NRError(RuntimeError):
@@ -121,6 +122,7 @@ def lib():
         L.nr_checkpoint8_write.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp]
         L.nr_checkpoint8_read.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, i32, vp]
         L.nr_ops_status.argtypes = [i32]
+        L.nr_ops_wait_limit.argtypes = [i64]
         for name in EXPORTS:
             if name not in ("nr_status_string", "nr_index_free", "nr_kernel_launches",
                             "nr_build_free") + sz:

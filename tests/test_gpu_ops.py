@@ -456,7 +456,9 @@ def test_offsets_past_32_bits(ops):
     dy[-200:] = ys
     dx, dw, db = ops.linear_backward(dy, x, w, z=z8, act="gelu")
     dxs, dws, dbs = ops.linear_backward(ys, tail, w, z=zs, act="gelu")
-    assert torch.equal(dx[-200:], dxs)
+    # a small batch's products may be summed in parts: the order is fixed for given sizes only
+    sx = (ys.double().abs() * 1.13) @ w.double().abs()
+    near(dx[-200:], dxs.double(), 2 * U[BF16] * dxs.double().abs() + 2 * (n + 16) * 2.0 ** -23 * sx, "dx")
     d = dws.double()
     # the same products in another order: 2^-8 for the rounding of dz and dw, as above
     mag = ys.double().abs().T @ tail.double().abs() * 1.13
