@@ -1,5 +1,6 @@
 // 8-bit activation checkpoints (neuroute_ops.h): groups of 32 columns of a row
-// share a power-of-two scale. A thread holds a group.
+// share a power-of-two scale. Bound by memory in both directions: a value's 2 or 4
+// bytes one way and 1 + 1/32 the other.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -7,40 +8,141 @@
 
 namespace {
 
-__global__ void __launch_bounds__(256)
-    write8_kernel(const void *x, int dtype, int64_t m, int64_t n, int64_t groups, int64_t x_ld,
-                  int8_t *codes, uint8_t *scales) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= m * groups) return;
-  const int64_t i = e / groups, c0 = (e - i * groups) * kOpsGroup;
-  float v[kOpsGroup];
-  uint32_t top = 0;
-#pragma unroll
-  for (int c = 0; c < kOpsGroup; ++c) {
-    v[c] = c0 + c < n ? load_any(x, i * x_ld + c0 + c, dtype) : 0.0f;
-    top = max(top, __float_as_uint(v[c]) & 0x7fffffffu);
+constexpr int kThreads = 256, kBlocks = 6, kBatch = 4;  // blocks an SM, rows at a time
+
+// eight values of a row as they lie in memory (vec: 16-byte accesses)
+template <typename T>
+struct Eight {
+  uint32_t r[sizeof(T) == 4 ? 8 : 4];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> read_eight(const T *p, bool vec, int count) {
+  Eight<T> o = {};
+  if (vec && count == 8) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
+    o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
+    if (sizeof(T) == 4) {
+      const uint4 b = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
+      o.r[4 % (sizeof(T) * 2)] = b.x, o.r[5 % (sizeof(T) * 2)] = b.y;
+      o.r[6 % (sizeof(T) * 2)] = b.z, o.r[7 % (sizeof(T) * 2)] = b.w;
+    }
+    return o;
   }
-  const uint32_t s = held8_scale(top);
-  const float up = held8_up(s);
-  scales[e] = (uint8_t)s;
 #pragma unroll
-  for (int c = 0; c < kOpsGroup; ++c) codes[e * kOpsGroup + c] = (int8_t)held8_code(v[c], up);
+  for (int q = 0; q < 8; ++q)
+    if (q < count) {
+      if (sizeof(T) == 4) o.r[q % (sizeof(T) * 2)] = __ldg(reinterpret_cast<const uint32_t *>(p) + q);
+      else o.r[q >> 1] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + q) << (16 * (q & 1));
+    }
+  return o;
+}
+// the fp32 bits of the largest magnitude: 16-bit types are ordered like their
+// bits without the sign
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Eight<T> &o) {
+  if (sizeof(T) == 4) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) top = max(top, o.r[q % (sizeof(T) * 2)] & 0x7fffffffu);
+    return top;
+  }
+  uint32_t top = o.r[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int q = 1; q < 4; ++q) top = __vmaxu2(top, o.r[q] & 0x7fff7fffu);
+  top = max(top & 0xffffu, top >> 16);
+  return __float_as_uint(unpack2(top, TypeCode<T>::code).x);
+}
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const Eight<T> &o, int p) {
+  if (sizeof(T) == 4)
+    return make_float2(__uint_as_float(o.r[2 * p % (sizeof(T) * 2)]), __uint_as_float(o.r[(2 * p + 1) % (sizeof(T) * 2)]));
+  return unpack2(o.r[p], TypeCode<T>::code);
 }
 
-__global__ void __launch_bounds__(256)
-    read8_kernel(const int8_t *codes, const uint8_t *scales, int64_t m, int64_t n, int64_t groups, int act,
-                 void *y, int dtype, int64_t y_ld) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= m * groups) return;
-  const int64_t i = e / groups, c0 = (e - i * groups) * kOpsGroup;
-  const float down = held8_down(scales[e]);
+// Threads of a block: x along a row (eight columns each, four threads a group),
+// y over rows; a thread takes kBatch rows at a time, all their loads first.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+    write8_kernel(const T *x, int vec, int64_t m, int n, int groups, int64_t x_ld, int8_t *codes, uint8_t *scales) {
+  const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int count = max(0, min(8, n - j));
+  const bool in = j < groups * kOpsGroup;
+  const int64_t step = (int64_t)gridDim.y * blockDim.y;
+  const unsigned lanes = 0xfu << ((threadIdx.y * blockDim.x + threadIdx.x) & 28);
+  for (int64_t i0 = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; i0 < m; i0 += step * kBatch) {
+    Eight<T> v[kBatch];
 #pragma unroll
-  for (int c = 0; c < kOpsGroup; ++c) {
-    if (c0 + c >= n) break;
-    float v = act_value((float)codes[e * kOpsGroup + c] * down, act);
-    if (dtype == NR_F16 && fabsf(v) > 65504.0f) v = copysignf(65504.0f, v);
-    store_any(y, i * y_ld + c0 + c, dtype, v);
+    for (int u = 0; u < kBatch; ++u)
+      v[u] = i0 + u * step < m && count > 0 ? read_eight<T>(x + (i0 + u * step) * x_ld + j, vec, count) : Eight<T>{};
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t i = i0 + u * step;
+      uint32_t top = largest<T>(v[u]);
+      top = max(top, __shfl_xor_sync(lanes, top, 1));
+      top = max(top, __shfl_xor_sync(lanes, top, 2));
+      const uint32_t s = held8_scale(top);
+      const float up = held8_up(s);
+      if (!in || i >= m) continue;
+      *reinterpret_cast<uint2 *>(codes + i * groups * kOpsGroup + j) =
+          make_uint2(held8_codes(pair_of<T>(v[u], 0), pair_of<T>(v[u], 1), up, s),
+                     held8_codes(pair_of<T>(v[u], 2), pair_of<T>(v[u], 3), up, s));
+      if ((threadIdx.x & 3) == 0) scales[i * groups + (j >> 5)] = (uint8_t)s;
+    }
   }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+    read8_kernel(const int8_t *codes, const uint8_t *scales, int64_t m, int n, int groups, int act, T *y, int vec,
+                 int64_t y_ld) {
+  const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  if (j >= n) return;
+  const int count = min(8, n - j);
+  const int64_t step = (int64_t)gridDim.y * blockDim.y;
+  for (int64_t i0 = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; i0 < m; i0 += step * kBatch) {
+    uint2 c[kBatch];
+    uint32_t s[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t i = min(i0 + u * step, m - 1);
+      c[u] = __ldg(reinterpret_cast<const uint2 *>(codes + i * groups * kOpsGroup + j));
+      s[u] = __ldg(scales + i * groups + (j >> 5));
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t i = i0 + u * step;
+      if (i >= m) break;
+      const float down = held8_down(s[u]);
+      float2 p[4];
+      held8_numbers(c[u].x, p[0], p[1]);
+      held8_numbers(c[u].y, p[2], p[3]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) p[q] = mul2(p[q], both(down));
+      if (act != NR_ACT_NONE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p[q] = make_float2(act_value(p[q].x, act), act_value(p[q].y, act));
+      }
+      if (TypeCode<T>::code == NR_F16 && s[u] >= 143u) {  // 64 x 2^10 stands for up to 65504: keep it finite; NaN stays
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          p[q].x = p[q].x > 65504.0f ? 65504.0f : p[q].x < -65504.0f ? -65504.0f : p[q].x;
+          p[q].y = p[q].y > 65504.0f ? 65504.0f : p[q].y < -65504.0f ? -65504.0f : p[q].y;
+        }
+      }
+      const float v[8] = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+      store8(y + i * y_ld, j, TypeCode<T>::code, vec, count, v);
+    }
+  }
+}
+
+// the block's shape and the grid: rows of few columns share a block
+void cut(int64_t m, int64_t n, int sms, dim3 &grid, dim3 &block) {
+  const int64_t segs = ceil_div(n, kOpsGroup) * 4;
+  unsigned bx = 4;
+  while (bx < (unsigned)kThreads && bx < segs) bx *= 2;
+  block = dim3(bx, kThreads / bx);
+  const int64_t gx = ceil_div(segs, bx), rows = ceil_div(m, block.y), most = ceil_div((int64_t)sms * kBlocks, gx);
+  grid = dim3((unsigned)gx, (unsigned)(rows < most ? rows : most));
 }
 
 bool valid(const void *codes, const void *scales, const void *v, int64_t m, int64_t n, int dtype) {
@@ -57,8 +159,18 @@ extern "C" nr_status nr_checkpoint8_write(const void *x, int dtype, int64_t m, i
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;
   const int64_t groups = ceil_div(n, kOpsGroup);
-  write8_kernel<<<(unsigned)ceil_div(m * groups, 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(
-      x, dtype, m, n, groups, x_ld, static_cast<int8_t *>(codes), static_cast<uint8_t *>(scales));
+  dim3 grid, block;
+  cut(m, n, nr_ops_sms(device), grid, block);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int vec = vec_ok(x, x_ld, dtype);
+  int8_t *c = static_cast<int8_t *>(codes);
+  uint8_t *sc = static_cast<uint8_t *>(scales);
+  if (dtype == NR_F32)
+    write8_kernel<<<grid, block, 0, s>>>(static_cast<const float *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
+  else if (dtype == NR_F16)
+    write8_kernel<<<grid, block, 0, s>>>(static_cast<const __half *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
+  else
+    write8_kernel<<<grid, block, 0, s>>>(static_cast<const __nv_bfloat16 *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }
@@ -70,8 +182,18 @@ extern "C" nr_status nr_checkpoint8_read(const void *codes, const void *scales, 
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;
   const int64_t groups = ceil_div(n, kOpsGroup);
-  read8_kernel<<<(unsigned)ceil_div(m * groups, 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(
-      static_cast<const int8_t *>(codes), static_cast<const uint8_t *>(scales), m, n, groups, act, y, dtype, y_ld);
+  dim3 grid, block;
+  cut(m, n, nr_ops_sms(device), grid, block);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int vec = vec_ok(y, y_ld, dtype);
+  const int8_t *c = static_cast<const int8_t *>(codes);
+  const uint8_t *sc = static_cast<const uint8_t *>(scales);
+  if (dtype == NR_F32)
+    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<float *>(y), vec, y_ld);
+  else if (dtype == NR_F16)
+    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<__half *>(y), vec, y_ld);
+  else
+    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<__nv_bfloat16 *>(y), vec, y_ld);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }

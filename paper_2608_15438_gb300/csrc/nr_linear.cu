@@ -57,58 +57,6 @@ struct Epilogue {
   int y_vec, z_vec, residual_vec;  // eight columns a 16-byte access (32 bytes in fp32)
 };
 
-__device__ __forceinline__ uint32_t pack2(float a, float b, int dtype) {
-  if (dtype == NR_F16) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-  }
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ float2 unpack2(uint32_t v, int dtype) {
-  if (dtype == NR_F16) return __half22float2(*reinterpret_cast<const __half2 *>(&v));
-  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&v));
-}
-
-// eight consecutive elements from (row pointer index) e on, `count` of them there
-__device__ __forceinline__ void load8(const void *p, int64_t e, int dtype, int vec, int count, float (&v)[8]) {
-  if (vec && count >= 8) {
-    if (dtype == NR_F32) {
-      const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e);
-      const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + e);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float2 f = unpack2(w[q], dtype);
-        v[2 * q] = f.x;
-        v[2 * q + 1] = f.y;
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = q < count ? load_any(p, e + q, dtype) : 0.0f;
-}
-__device__ __forceinline__ void store8(void *p, int64_t e, int dtype, int vec, int count, const float (&v)[8]) {
-  if (vec && count >= 8) {
-    if (dtype == NR_F32) {
-      float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(p) + e);
-      d[0] = make_float4(v[0], v[1], v[2], v[3]);
-      d[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + e) =
-          make_uint4(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype), pack2(v[4], v[5], dtype), pack2(v[6], v[7], dtype));
-    }
-    return;
-  }
-#pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (q < count) store_any(p, e + q, dtype, v[q]);
-}
-
 // Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'). The four
 // threads of a group of 32 columns call it together (lanes 4 a .. 4 a + 3 of a
 // warp, in column order), row_ok false for rows past the end.
@@ -129,11 +77,12 @@ __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int64_t j,
       const float up = held8_up(sc);
       const int64_t groups = (E.n + kOpsGroup - 1) / kOpsGroup;
       if (row_ok && j < groups * kOpsGroup) {
-        uint32_t c[2] = {0u, 0u};
+        float u[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (q < count) c[q >> 2] |= ((uint32_t)held8_code(v[q], up) & 0xffu) << (8 * (q & 3));
-        *reinterpret_cast<uint2 *>(static_cast<int8_t *>(E.z) + i * groups * kOpsGroup + j) = make_uint2(c[0], c[1]);
+        for (int q = 0; q < 8; ++q) u[q] = q < count ? v[q] : 0.0f;
+        *reinterpret_cast<uint2 *>(static_cast<int8_t *>(E.z) + i * groups * kOpsGroup + j) =
+            make_uint2(held8_codes(make_float2(u[0], u[1]), make_float2(u[2], u[3]), up, sc),
+                       held8_codes(make_float2(u[4], u[5]), make_float2(u[6], u[7]), up, sc));
         if ((j & (kOpsGroup - 1)) == 0) E.z_scale[i * groups + (j >> 5)] = (uint8_t)sc;
       }
     } else if (count > 0) {
@@ -496,9 +445,14 @@ __device__ __forceinline__ void saved8(const Saved &s, int64_t i, int64_t j, int
   }
   const uint2 c = *reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(s.p) + i * s.groups * kOpsGroup + j);
   const float down = held8_down(s.scale[i * s.groups + (j >> 5)]);
+  float2 p[4];
+  held8_numbers(c.x, p[0], p[1]);
+  held8_numbers(c.y, p[2], p[3]);
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
-    v[q] = (float)(int8_t)((q < 4 ? c.x : c.y) >> (8 * (q & 3))) * down;
+  for (int q = 0; q < 4; ++q) {
+    v[2 * q] = p[q].x * down;
+    v[2 * q + 1] = p[q].y * down;
+  }
 }
 
 // dz = dy act'(z) rounded to dtype (unless dz is null), and the column sums of
@@ -720,10 +674,6 @@ cudaError_t pack(const void *src, int64_t ld, int64_t rows, int64_t cols, void *
   pack_kernel<<<(unsigned)ceil_div(rows * (d_ld / 8), 256), 256, 0, s>>>(static_cast<const uint16_t *>(src), ld, rows,
                                                                          cols, static_cast<uint16_t *>(dst), d_ld);
   return cudaGetLastError();
-}
-
-bool vec_ok(const void *p, int64_t ld, int64_t dtype) {
-  return aligned16(p) && ld * (int64_t)type_bytes(dtype) % 16 == 0;
 }
 
 bool valid(const nr_linear *a, bool backward) {

@@ -1,5 +1,23 @@
-// Layer norm of residual encoders (neuroute_ops.h), simple form: a block a row;
-// the parameters' gradients by a block for every 32 columns.
+// Layer norm of residual encoders (neuroute_ops.h).
+//   forward   mean = sum x / n, rstd = (sum (x - mean)^2 / n + eps)^-1/2,
+//             y = (x - mean) rstd weight + bias
+//   backward  xh = (x - mean) rstd, g = dy weight; dx = rstd (g - mean(g) -
+//             xh mean(g xh)) + residual gradient; dweight = sum_m dy xh,
+//             dbias = sum_m dy
+//
+// Both are bound by memory: forward reads x and writes y, backward reads dy and
+// x (and the residual's gradient) and writes dx, each once. A row is held in the
+// registers of some lanes, a warp or a block, so that the statistics' second
+// pass (the deviations from the mean, which loses nothing to cancellation) and
+// the output need no second read; several rows at a time keep enough bytes in
+// flight. Persistent grids walk the rows; in the backward pass each thread
+// keeps the parameters' sums of its columns in registers over all its rows, and
+// a second kernel adds the blocks' sums in order.
+//
+// A thread's columns: eight consecutive ones at a time where every matrix
+// allows 16-byte accesses (or x is a checkpoint), else single ones a group's width
+// apart, so that a group's accesses stay contiguous. Rows longer than 16384
+// are read again from memory by a block a row (the long_ kernels).
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -7,103 +25,616 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-
 // values of a type, or a checkpoint's codes and scales
 struct Rows {
   const void *p;
   const uint8_t *scale;
   int64_t ld;
-  int dtype;
   int64_t groups;
 };
-__device__ __forceinline__ float row_at(const Rows &s, int64_t i, int64_t j) {
-  if (!s.scale) return load_any(s.p, i * s.ld + j, s.dtype);
-  return (float)static_cast<const int8_t *>(s.p)[i * s.groups * kOpsGroup + j] *
-         held8_down(s.scale[i * s.groups + j / kOpsGroup]);
+
+struct Norm {
+  int64_t m, n;
+  Rows x;
+  const void *weight, *bias;
+  int w_dtype;
+  float eps;
+  void *y;
+  int64_t y_ld;
+  float *mean, *rstd;
+  const void *dy;
+  int64_t dy_ld;
+  const void *dres;
+  int64_t dres_ld;
+  void *dx;
+  int64_t dx_ld;
+  float *parts;  // [blocks][2][n]: the blocks' sums for dweight, dbias
+  int eights;    // a thread's columns come in eights
+  int vec;       // and every matrix takes 16-byte accesses
+  int w_vec;     // as do weight and bias
+};
+
+// A thread's v-th eight elements of a row as they lie in memory.
+template <typename T>
+struct Raw {
+  uint32_t r[sizeof(T) == 4 ? 8 : 4];
+};
+
+// the column of element q of the thread's v-th eight, of a group of TPR threads
+// (0: of `width`)
+template <int TPR>
+__device__ __forceinline__ int column(int eights, int v, int q, int t, int width = TPR) {
+  const int w = TPR ? TPR : width;
+  return eights ? (v * w + t) * 8 + q : (v * 8 + q) * w + t;
 }
 
-__device__ __forceinline__ float block_sum(float v) {
-  __shared__ float part[kThreads / 32];
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+template <int TPR, typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, int width = TPR) {
+  Raw<T> o = {};
+  const int c = column<TPR>(eights, v, 0, t, width);
+  if (vec) {  // n is a multiple of 8
+    if (c < n) {
+      const uint4 *p = reinterpret_cast<const uint4 *>(row + c);
+      const uint4 a = __ldg(p);
+      o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
+      if (sizeof(T) == 4) {
+        const uint4 b = __ldg(p + 1);
+        o.r[4 % (sizeof(T) * 2)] = b.x, o.r[5 % (sizeof(T) * 2)] = b.y;
+        o.r[6 % (sizeof(T) * 2)] = b.z, o.r[7 % (sizeof(T) * 2)] = b.w;
+      }
+    }
+    return o;
+  }
+  // loads without branches, so that all are under way at once
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int cq = eights ? c + q : c + q * (TPR ? TPR : width), at = min(cq, n - 1);
+    if (sizeof(T) == 4) {
+      const uint32_t u = __ldg(reinterpret_cast<const uint32_t *>(row) + at);
+      o.r[q % (sizeof(T) * 2)] = cq < n ? u : 0u;
+    } else {
+      const uint32_t u = __ldg(reinterpret_cast<const uint16_t *>(row) + at);
+      o.r[q >> 1] |= cq < n ? u << (16 * (q & 1)) : 0u;
+    }
+  }
+  return o;
+}
+// elements 2 p and 2 p + 1
+template <typename T>
+__device__ __forceinline__ float2 raw_pair(const Raw<T> &o, int p) {
+  if (sizeof(T) == 4)
+    return make_float2(__uint_as_float(o.r[2 * p % (sizeof(T) * 2)]), __uint_as_float(o.r[(2 * p + 1) % (sizeof(T) * 2)]));
+  return unpack2(o.r[p], TypeCode<T>::code);
+}
+// x, which may be a checkpoint: then the codes as numbers of T, exactly, and
+// their scale
+template <int TPR, typename T>
+__device__ __forceinline__ Raw<T> load_held(const Rows &x, int64_t i, int v, int t, int n, float &scale, int width = TPR) {
+  Raw<T> o = {};
+  scale = 1.0f;
+  const int c = column<TPR>(1, v, 0, t, width);
+  if (c < n) {
+    const uint2 a = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(x.p) + i * x.groups * kOpsGroup + c));
+    scale = held8_down(__ldg(x.scale + i * x.groups + (c >> 5)));
+    float2 p[4];
+    held8_numbers(a.x, p[0], p[1]);
+    held8_numbers(a.y, p[2], p[3]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (sizeof(T) == 4) {
+        o.r[2 * q % (sizeof(T) * 2)] = __float_as_uint(p[q].x);
+        o.r[(2 * q + 1) % (sizeof(T) * 2)] = __float_as_uint(p[q].y);
+      } else {
+        o.r[q] = pack2(p[q].x, p[q].y, TypeCode<T>::code);
+      }
+    }
+  }
+  return o;
+}
+template <int TPR, typename T>
+__device__ __forceinline__ void store_row(T *row, int eights, bool vec, int v, int t, int n, const float2 (&p)[4], int width = TPR) {
+  const float o[8] = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+  const int c = column<TPR>(eights, v, 0, t, width);
+  if (vec) {
+    if (c < n) store8(row, c, TypeCode<T>::code, 1, 8, o);
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int cq = eights ? c + q : c + q * (TPR ? TPR : width);
+    if (cq < n) row[cq] = from_f32<T>(o[q]);
+  }
+}
+// eight of the weights (or biases) as a thread's columns need them
+template <int TPR>
+__device__ __forceinline__ void load_w(const void *p, int dtype, float none, int eights, bool vec, int v, int t, int n,
+                                       float2 (&w)[4], int width = TPR) {
+  float o[8];
+  const int c = column<TPR>(eights, v, 0, t, width);
+  if (p && vec) {
+    load8(p, c < n ? c : 0, dtype, 1, 8, o);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int cq = eights ? c + q : c + q * (TPR ? TPR : width);
+      o[q] = p && cq < n ? load_any(p, cq, dtype) : none;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w[q] = make_float2(o[2 * q], o[2 * q + 1]);
+}
+
+// Keeps what was loaded or converted before it from being held in registers for
+// reuse after it: the registers buy more rows in flight.
+__device__ __forceinline__ void forget() { asm volatile("" ::: "memory"); }
+template <typename T>
+__device__ __forceinline__ void forget(Raw<T> &o) {
+#pragma unroll
+  for (int k = 0; k < (sizeof(T) == 4 ? 8 : 4); ++k) asm volatile("" : "+r"(o.r[k]));
+}
+
+// ------------------------------------------------------------ sums over a row's threads
+// TPR lanes of a warp
+template <int TPR, int K>
+__device__ __forceinline__ void lane_sums(float (&v)[K]) {
+#pragma unroll
+  for (int o = TPR / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+}
+// All threads of a block: K sums (a power of two up to 8). A warp halves the
+// values it carries at every exchange, so K sums take K + 5 - log2 K
+// exchanges at most; the warps' sums are added in order by every thread. `turn`
+// alternates between two buffers, so that one barrier a call is enough.
+constexpr int kWarpsMax = 16;
+template <int K>
+struct BlockSums {
+  float part[2][kWarpsMax][K < 4 ? 4 : K];
+};
+template <int K>
+__device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int turn) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  float u[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) u[k] = v[k];
+  int o = 16;
+#pragma unroll
+  for (int h = K / 2; h >= 1; h >>= 1, o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int k = 0; k < h; ++k) {
+      const float send = up ? u[k] : u[k + h], keep = up ? u[k + h] : u[k];
+      u[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  }
+  for (; o > 0; o >>= 1) u[0] += __shfl_xor_sync(0xffffffffu, u[0], o);
+  constexpr int kLanes = 32 / K;  // lanes that hold the same sum
+  if (lane % kLanes == 0) S.part[turn & 1][warp][lane / kLanes] = u[0];
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0.0f;
-  for (int w = 0; w < kThreads / 32; ++w) v += part[w];
-  return v;
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = 0.0f;
+  for (int w = 0; w < warps; ++w)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += S.part[turn & 1][w][k];
 }
 
-__global__ void __launch_bounds__(kThreads)
-    norm_forward_kernel(Rows x, int64_t n, const void *weight, const void *bias, int w_dtype, float eps, void *y,
-                        int64_t y_ld, int dtype, float *mean_out, float *rstd_out) {
-  const int64_t i = blockIdx.x;
-  float s = 0.0f;
-  for (int64_t j = threadIdx.x; j < n; j += kThreads) s += row_at(x, i, j);
-  const float mean = block_sum(s) / (float)n;
-  s = 0.0f;
-  for (int64_t j = threadIdx.x; j < n; j += kThreads) {
-    const float d = row_at(x, i, j) - mean;
-    s = fmaf(d, d, s);
+// ------------------------------------------------------------ rows in registers
+// R rows from i on of a group of TPR threads (0: the block), V eights a thread:
+// centred, with their means and reciprocal deviations, then written. Rows from
+// m on are skipped (they hold zeros).
+template <int TPR, int V, int R, bool VEC, typename T>
+struct Forward {
+  float2 x[R][V][4];
+  float mean[R], rstd[R];
+
+  template <typename Sums>
+  __device__ __forceinline__ void statistics(const Norm &N, int64_t i, int t, int eights, int width, Sums sums) {
+    const int n = (int)N.n;
+    const float inv = 1.0f / (float)n;
+    Raw<T> raw[R][V];
+    if (!N.x.scale) {
+      const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, n, width) : Raw<T>{};
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[r][v][q] = raw_pair(raw[r][v], q);
+    } else {
+      float scale[R][V];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[r][v] = load_held<TPR, T>(N.x, min(i + r, N.m - 1), v, t, n, scale[r][v], width);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[r][v][q] = mul2(raw_pair(raw[r][v], q), both(scale[r][v]));
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float2 s = both(0.0f);  // zeros past the row's end
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s = add2(s, x[r][v][q]);
+      mean[r] = s.x + s.y;
+    }
+    sums(mean);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean[r] *= inv;
+      float2 s = both(0.0f);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const bool in = column<TPR>(eights, v, 0, t, width) < n;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float2 d = add2(x[r][v][q], both(-mean[r]));
+          if (VEC) {
+            if (!in) d = both(0.0f);
+          } else {
+            if (column<TPR>(eights, v, 2 * q, t, width) >= n) d.x = 0.0f;
+            if (column<TPR>(eights, v, 2 * q + 1, t, width) >= n) d.y = 0.0f;
+          }
+          x[r][v][q] = d;
+          s = fma2(d, d, s);
+        }
+      }
+      rstd[r] = s.x + s.y;
+    }
+    sums(rstd);
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = 1.0f / sqrtf(fmaf(rstd[r], inv, N.eps));
   }
-  const float rstd = 1.0f / sqrtf(block_sum(s) / (float)n + eps);
-  for (int64_t j = threadIdx.x; j < n; j += kThreads) {
-    const float g = weight ? load_any(weight, j, w_dtype) : 1.0f, b = bias ? load_any(bias, j, w_dtype) : 0.0f;
-    store_any(y, i * y_ld + j, dtype, fmaf((row_at(x, i, j) - mean) * rstd, g, b));
+
+  __device__ __forceinline__ void write(const Norm &N, int64_t i, int v, int t, int eights, int width,
+                                        const float2 (&w)[4], const float2 (&b)[4]) {
+    T *y = static_cast<T *>(N.y) + i * N.y_ld;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (i + r >= N.m) break;
+      float2 o[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) o[q] = fma2(mul2(x[r][v][q], both(rstd[r])), w[q], b[q]);
+      store_row<TPR, T>(y + r * N.y_ld, eights, VEC, v, t, (int)N.n, o, width);
+    }
   }
-  if (mean_out && threadIdx.x == 0) {
-    mean_out[i] = mean;
-    rstd_out[i] = rstd;
+  __device__ __forceinline__ void write_statistics(const Norm &N, int64_t i) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (i + r < N.m) {
+        N.mean[i + r] = mean[r];
+        N.rstd[i + r] = rstd[r];
+      }
+  }
+};
+
+// The same for the backward pass: x and dy stay as they lie in memory, and are
+// converted twice.
+template <int TPR, int V, int R, bool VEC, typename T>
+struct Backward {
+  Raw<T> x[R][V], dy[R][V];
+  float scale[R][V], shift[R], rstd[R];  // xh = x scale + shift
+  float s[2 * R];                        // sum g, sum g xh of the thread's columns, then of the rows
+
+  __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int width) {
+    const int n = (int)N.n;
+    const T *pd = static_cast<const T *>(N.dy) + i * N.dy_ld, *px = static_cast<const T *>(N.x.p) + i * N.x.ld;
+    // one branch around all loads, so that they are under way together; rows past
+    // the end hold zeros and add nothing
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        dy[r][v] = i + r < N.m ? load_raw<TPR, T>(pd + r * N.dy_ld, eights, VEC, v, t, n, width) : Raw<T>{};
+    if (N.x.scale) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[r][v] = load_held<TPR, T>(N.x, min(i + r, N.m - 1), v, t, n, scale[r][v], width);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          x[r][v] = i + r < N.m ? load_raw<TPR, T>(px + r * N.x.ld, eights, VEC, v, t, n, width) : Raw<T>{};
+          scale[r][v] = 1.0f;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      shift[r] = i + r < N.m ? N.mean[i + r] : 0.0f;
+      rstd[r] = i + r < N.m ? N.rstd[i + r] : 0.0f;
+      s[2 * r] = s[2 * r + 1] = 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      shift[r] *= -rstd[r];
+#pragma unroll
+      for (int v = 0; v < V; ++v) scale[r][v] *= rstd[r];
+    }
+  }
+  __device__ __forceinline__ void add(int v, const float2 (&w)[4], float2 (&dw)[4], float2 (&db)[4]) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float2 s1 = both(0.0f), s2 = both(0.0f);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        // dy is zero past the row's end, and xh finite where the row is
+        const float2 d = raw_pair(dy[r][v], q), g = mul2(d, w[q]);
+        const float2 xh = fma2(raw_pair(x[r][v], q), both(scale[r][v]), both(shift[r]));
+        s1 = add2(s1, g);
+        s2 = fma2(g, xh, s2);
+        db[q] = add2(db[q], d);
+        dw[q] = fma2(d, xh, dw[q]);
+      }
+      s[2 * r] += s1.x + s1.y;
+      s[2 * r + 1] += s2.x + s2.y;
+    }
+  }
+  __device__ __forceinline__ void write(const Norm &N, int64_t i, int v, int t, int eights, int width,
+                                        const float2 (&w)[4]) {
+    const float inv = 1.0f / (float)(int)N.n;
+    const T *res = static_cast<const T *>(N.dres) + i * N.dres_ld;
+    T *dx = static_cast<T *>(N.dx) + i * N.dx_ld;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (i + r >= N.m) break;
+      forget(x[r][v]);
+      forget(dy[r][v]);
+      const float2 m1 = both(-s[2 * r] * inv * rstd[r]), m2 = both(-s[2 * r + 1] * inv * rstd[r]);
+      float2 o[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 xh = fma2(raw_pair(x[r][v], q), both(scale[r][v]), both(shift[r]));
+        o[q] = fma2(xh, m2, fma2(mul2(raw_pair(dy[r][v], q), w[q]), both(rstd[r]), m1));
+      }
+      if (N.dres) {
+        const Raw<T> rr = load_raw<TPR, T>(res + r * N.dres_ld, eights, VEC, v, t, (int)N.n, width);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = add2(o[q], raw_pair(rr, q));
+      }
+      store_row<TPR, T>(dx + r * N.dx_ld, eights, VEC, v, t, (int)N.n, o, width);
+    }
+  }
+};
+
+// ------------------------------------------------------------ a row in a warp
+// Blocks of 128: groups of TPR lanes hold R rows each, V eights of them a thread.
+constexpr int kWarpThreads = 128;
+
+template <int TPR, int V, bool VEC, typename T>
+__global__ void __launch_bounds__(kWarpThreads, V == 6 ? 5 : 4) warp_forward_kernel(const Norm N) {
+  constexpr int R = V == 6 ? 1 : V == 3 ? 2 : 4, kGroups = kWarpThreads / TPR;
+  const int t = threadIdx.x % TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
+  const bool w_vec = VEC && N.w_vec;
+  float2 w[4], b[4];  // V = 1: a thread's own, kept
+  if (V == 1) {
+    load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, w_vec, 0, t, n, w);
+    load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, w_vec, 0, t, n, b);
+  }
+  // a block's groups take the same number of turns, so that shuffles are complete
+  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
+    const int64_t i = i0 + threadIdx.x / TPR * R;
+    Forward<TPR, V, R, VEC, T> F;
+    F.statistics(N, i, t, eights, TPR, [](float(&v)[R]) { lane_sums<TPR, R>(v); });
+    if (V > 1) forget();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (V > 1) {
+        load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w);
+        load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, w_vec, v, t, n, b);
+      }
+      F.write(N, i, v, t, eights, TPR, w, b);
+    }
+    if (N.mean && t == 0) F.write_statistics(N, i);
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
-    norm_dx_kernel(const void *dy, int64_t dy_ld, Rows x, int64_t n, const void *weight, int w_dtype,
-                   const float *mean, const float *rstd, const void *dres, int64_t dres_ld, void *dx, int64_t dx_ld,
-                   int dtype) {
-  const int64_t i = blockIdx.x;
-  const float mu = mean[i], rs = rstd[i];
-  float s1 = 0.0f, s2 = 0.0f;
-  for (int64_t j = threadIdx.x; j < n; j += kThreads) {
-    const float g = load_any(dy, i * dy_ld + j, dtype) * (weight ? load_any(weight, j, w_dtype) : 1.0f);
-    s1 += g;
-    s2 = fmaf(g, (row_at(x, i, j) - mu) * rs, s2);
+// Up to 256 columns: V = 1, four rows a group (two in fp32).
+template <int TPR, bool VEC, typename T>
+__global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const Norm N) {
+  constexpr int R = sizeof(T) == 4 ? 2 : 4, kGroups = kWarpThreads / TPR;
+  __shared__ float sums[2][TPR * 8];
+  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
+  float2 w[4], dw[4] = {}, db[4] = {};
+  load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC && N.w_vec, 0, t, n, w);
+  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
+    const int64_t i = i0 + group * R;
+    Backward<TPR, 1, R, VEC, T> G;
+    G.load(N, i, t, eights, TPR);
+    G.add(0, w, dw, db);
+    lane_sums<TPR, 2 * R>(G.s);
+    G.write(N, i, 0, t, eights, TPR, w);
   }
-  const float m1 = block_sum(s1) / (float)n, m2 = block_sum(s2) / (float)n;
-  for (int64_t j = threadIdx.x; j < n; j += kThreads) {
-    const float g = load_any(dy, i * dy_ld + j, dtype) * (weight ? load_any(weight, j, w_dtype) : 1.0f);
-    float d = rs * (g - m1 - (row_at(x, i, j) - mu) * rs * m2);
-    if (dres) d += load_any(dres, i * dres_ld + j, dtype);
-    store_any(dx, i * dx_ld + j, dtype, d);
+  if (!N.parts) return;
+  float *part = N.parts + (int64_t)blockIdx.x * 2 * N.n;
+  for (int g = 0; g < kGroups; ++g) {  // the groups in order
+    if (group == g) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int c = column<TPR>(eights, 0, q, t);
+        float a = q & 1 ? dw[q >> 1].y : dw[q >> 1].x, e = q & 1 ? db[q >> 1].y : db[q >> 1].x;
+        if (g > 0) {
+          a += sums[0][t * 8 + q];
+          e += sums[1][t * 8 + q];
+        }
+        sums[0][t * 8 + q] = a;
+        sums[1][t * 8 + q] = e;
+        if (g + 1 == kGroups && c < n) {
+          part[c] = a;
+          part[n + c] = e;
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
+// ------------------------------------------------------------ a row in a block
+// The block has just the threads that a row's eights need; R rows at a time.
+template <int V, int R, int THREADS, bool VEC, typename T>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) block_forward_kernel(const Norm N) {
+  __shared__ BlockSums<R> S;
+  const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
+  const bool w_vec = VEC && N.w_vec;
+  int turn = 0;
+  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
+    Forward<0, V, R, VEC, T> F;
+    F.statistics(N, i, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++); });
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float2 w[4], b[4];
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
+      load_w<0>(N.bias, N.w_dtype, 0.0f, eights, w_vec, v, t, n, b, width);
+      F.write(N, i, v, t, eights, width, w, b);
+    }
+    if (N.mean && t == 0) F.write_statistics(N, i);
+  }
+}
+
+template <int V, int R, int THREADS, bool VEC, typename T>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) block_backward_kernel(const Norm N) {
+  __shared__ BlockSums<2 * R> S;
+  const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
+  const bool w_vec = VEC && N.w_vec;
+  float2 dw[V][4] = {}, db[V][4] = {};
+  int turn = 0;
+  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
+    Backward<0, V, R, VEC, T> G;
+    G.load(N, i, t, eights, width);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float2 w[4];
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
+      G.add(v, w, dw[v], db[v]);
+    }
+    block_sums<2 * R>(G.s, S, turn++);
+    forget();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float2 w[4];
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
+      G.write(N, i, v, t, eights, width, w);
+    }
+  }
+  if (!N.parts) return;
+  float *part = N.parts + (int64_t)blockIdx.x * 2 * N.n;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int c = column<0>(eights, v, q, t, width);
+      if (c >= n) continue;
+      part[c] = q & 1 ? dw[v][q >> 1].y : dw[v][q >> 1].x;
+      part[n + c] = q & 1 ? db[v][q >> 1].y : db[v][q >> 1].x;
+    }
+}
+
+// dweight, dbias: the blocks' sums, 32 columns a block, eight rows of parts at a time
 __global__ void __launch_bounds__(256)
-    norm_dparam_kernel(const void *dy, int64_t dy_ld, Rows x, int64_t m, int64_t n, const float *mean,
-                       const float *rstd, int dtype, void *dweight, void *dbias, int w_dtype) {
+    norm_params_kernel(const float *parts, int count, int64_t n, void *dweight, void *dbias, int dtype) {
+  __shared__ float sums[8][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t e = (int64_t)blockIdx.x * 32 + c;  // into [2][n]
+  float s = 0.0f;
+  if (e < 2 * n) {
+#pragma unroll 8
+    for (int p = r; p < count; p += 8) s += parts[(int64_t)p * 2 * n + e];
+  }
+  sums[r][c] = s;
+  __syncthreads();
+  if (r != 0 || e >= 2 * n) return;
+  for (int q = 1; q < 8; ++q) s += sums[q][c];
+  store_any(e < n ? dweight : dbias, e < n ? e : e - n, dtype, s);
+}
+
+// ------------------------------------------------------------ rows past 16384
+constexpr int kLong = 16384, kLongThreads = 512;
+
+__device__ __forceinline__ float long_x(const Rows &x, int64_t i, int64_t j, int dtype) {
+  if (!x.scale) return load_any(x.p, i * x.ld + j, dtype);
+  return (float)static_cast<const int8_t *>(x.p)[i * x.groups * kOpsGroup + j] *
+         held8_down(x.scale[i * x.groups + (j >> 5)]);
+}
+
+__global__ void __launch_bounds__(kLongThreads) long_forward_kernel(const Norm N, int dtype) {
+  __shared__ BlockSums<1> S;
+  const int64_t i = blockIdx.x;
+  float s[1] = {0.0f};
+  for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) s[0] += long_x(N.x, i, j, dtype);
+  block_sums<1>(s, S, 0);
+  const float mean = s[0] / (float)N.n;
+  s[0] = 0.0f;
+  for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
+    const float d = long_x(N.x, i, j, dtype) - mean;
+    s[0] = fmaf(d, d, s[0]);
+  }
+  block_sums<1>(s, S, 1);
+  const float rstd = 1.0f / sqrtf(s[0] / (float)N.n + N.eps);
+  for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
+    const float w = N.weight ? load_any(N.weight, j, N.w_dtype) : 1.0f, b = N.bias ? load_any(N.bias, j, N.w_dtype) : 0.0f;
+    store_any(N.y, i * N.y_ld + j, dtype, fmaf((long_x(N.x, i, j, dtype) - mean) * rstd, w, b));
+  }
+  if (N.mean && threadIdx.x == 0) {
+    N.mean[i] = mean;
+    N.rstd[i] = rstd;
+  }
+}
+
+__global__ void __launch_bounds__(kLongThreads) long_dx_kernel(const Norm N, int dtype) {
+  __shared__ BlockSums<2> S;
+  const int64_t i = blockIdx.x;
+  const float mean = N.mean[i], rstd = N.rstd[i];
+  float s[2] = {0.0f, 0.0f};
+  for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
+    const float g = load_any(N.dy, i * N.dy_ld + j, dtype) * (N.weight ? load_any(N.weight, j, N.w_dtype) : 1.0f);
+    s[0] += g;
+    s[1] = fmaf(g, (long_x(N.x, i, j, dtype) - mean) * rstd, s[1]);
+  }
+  block_sums<2>(s, S, 0);
+  const float m1 = s[0] / (float)N.n, m2 = s[1] / (float)N.n;
+  for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
+    const float g = load_any(N.dy, i * N.dy_ld + j, dtype) * (N.weight ? load_any(N.weight, j, N.w_dtype) : 1.0f);
+    float d = rstd * (g - m1 - (long_x(N.x, i, j, dtype) - mean) * rstd * m2);
+    if (N.dres) d += load_any(N.dres, i * N.dres_ld + j, dtype);
+    store_any(N.dx, i * N.dx_ld + j, dtype, d);
+  }
+}
+
+// 32 columns and every gridDim.y-th eight rows a block -> parts
+__global__ void __launch_bounds__(256) long_params_kernel(const Norm N, int dtype) {
   __shared__ float pw[8][33], pb[8][33];
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
   const int64_t j = (int64_t)blockIdx.x * 32 + c;
   float w = 0.0f, b = 0.0f;
-  if (j < n)
-    for (int64_t i = r; i < m; i += 8) {
-      const float v = load_any(dy, i * dy_ld + j, dtype);
-      b += v;
-      w = fmaf(v, (row_at(x, i, j) - mean[i]) * rstd[i], w);
+  if (j < N.n)
+    for (int64_t i = (int64_t)blockIdx.y * 8 + r; i < N.m; i += (int64_t)gridDim.y * 8) {
+      const float d = load_any(N.dy, i * N.dy_ld + j, dtype);
+      b += d;
+      w = fmaf(d, (long_x(N.x, i, j, dtype) - N.mean[i]) * N.rstd[i], w);
     }
   pw[r][c] = w;
   pb[r][c] = b;
   __syncthreads();
-  if (r == 0 && j < n) {
-    for (int q = 1; q < 8; ++q) {
-      w += pw[q][c];
-      b += pb[q][c];
-    }
-    store_any(dweight, j, w_dtype, w);
-    store_any(dbias, j, w_dtype, b);
+  if (r != 0 || j >= N.n) return;
+  for (int q = 1; q < 8; ++q) {
+    w += pw[q][c];
+    b += pb[q][c];
   }
+  N.parts[(int64_t)blockIdx.y * 2 * N.n + j] = w;
+  N.parts[(int64_t)blockIdx.y * 2 * N.n + N.n + j] = b;
 }
 
+// ------------------------------------------------------------ host
 bool valid(const nr_layer_norm *a, bool backward) {
   if (!a || a->m < 0 || a->m > kOpsMaxRows || a->n < 1 || a->n > kOpsMaxCols) return false;
   if (a->dtype < NR_F32 || a->dtype > NR_BF16 || (a->w_dtype != a->dtype && a->w_dtype != NR_F32)) return false;
@@ -114,9 +645,111 @@ bool valid(const nr_layer_norm *a, bool backward) {
          (a->m == 0 || (a->dy && a->mean && a->rstd && a->dx && a->dx_ld >= a->n));
 }
 
-Rows rows_of(const nr_layer_norm *a) {
-  return {a->x, static_cast<const uint8_t *>(a->x_scale), a->x_ld, (int)a->dtype, ceil_div(a->n, kOpsGroup)};
+Norm norm_of(const nr_layer_norm *a, bool backward) {
+  Norm N = {};
+  N.m = a->m;
+  N.n = a->n;
+  N.x = {a->x, static_cast<const uint8_t *>(a->x_scale), a->x_ld, ceil_div(a->n, kOpsGroup)};
+  N.weight = a->weight;
+  N.bias = a->bias;
+  N.w_dtype = (int)a->w_dtype;
+  N.eps = (float)a->eps;
+  N.y = a->y;
+  N.y_ld = a->y_ld;
+  N.mean = a->mean;
+  N.rstd = a->rstd;
+  N.dy = a->dy;
+  N.dy_ld = a->dy_ld;
+  N.dres = a->residual_grad;
+  N.dres_ld = a->residual_grad_ld;
+  N.dx = a->dx;
+  N.dx_ld = a->dx_ld;
+  const int64_t dt = a->dtype;
+  bool vec = a->n % 8 == 0 && (a->x_scale || vec_ok(a->x, a->x_ld, dt));
+  if (backward)
+    vec = vec && vec_ok(a->dy, a->dy_ld, dt) && vec_ok(a->dx, a->dx_ld, dt) &&
+          (!a->residual_grad || vec_ok(a->residual_grad, a->residual_grad_ld, dt));
+  else
+    vec = vec && vec_ok(a->y, a->y_ld, dt);
+  N.vec = vec;
+  N.eights = vec || a->x_scale;
+  N.w_vec = N.eights && a->n % 8 == 0 && vec_ok(a->weight, 8, a->w_dtype) && vec_ok(a->bias, 8, a->w_dtype);
+  return N;
 }
+
+// How a row is held. Warps (tpr lanes a row, v eights a thread): forward up to
+// 1536 columns, where a row's sums cost five exchanges and no barrier;
+// backward up to 256, as the parameters' sums are 16 registers an eight and
+// leave too few rows in flight beyond. Fewer lanes take rows of 64 and 128, so that
+// none is idle. Blocks (tpr 0, v eights a thread, `threads` of them): up to
+// 16384. Longer rows: threads 0.
+struct Shape {
+  int tpr, v, threads;
+};
+Shape shape_of(int64_t n, bool vec, bool backward) {
+  if (n <= 256) return {vec && n <= 64 ? 8 : vec && n <= 128 ? 16 : 32, 1, kWarpThreads};
+  if (!backward && n <= 768) return {32, 3, kWarpThreads};
+  if (!backward && n <= 1536) return {32, 6, kWarpThreads};
+  if (n > kLong) return {0, 0, 0};
+  const int v = n <= (backward ? 2048 : 4096) ? 1 : n <= 8192 ? 2 : 4;
+  return {0, v, (int)round_up(ceil_div(n, 8 * v), 32)};
+}
+
+// Blocks of a persistent grid: those the registers allow at once, by sizes alone,
+// so that the order of the parameters' sums is fixed.
+int block_count(const Shape &s, int64_t m, bool backward, int sms) {
+  int per_sm, rows;
+  if (s.tpr) {
+    per_sm = s.v == 6 ? 5 : 4;
+    rows = kWarpThreads / s.tpr;
+  } else {
+    per_sm = s.threads <= 256 && s.v == 1 ? 768 / s.threads : (s.v == 4 || backward ? 512 : 1024) / s.threads;
+    rows = 1;
+  }
+  const int64_t need = ceil_div(m, rows), most = (int64_t)sms * per_sm;
+  return (int)(need < most ? need : most);
+}
+
+// rows at a time of a block with one eight a thread: what 80 registers hold
+template <bool VEC, typename T>
+constexpr int block_rows() { return VEC && sizeof(T) == 2 ? 4 : 2; }
+
+template <bool VEC, typename T>
+cudaError_t forward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
+  const int th = s.threads;
+  if (s.tpr == 8) warp_forward_kernel<8, 1, true, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_forward_kernel<16, 1, true, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr && s.v == 1) warp_forward_kernel<32, 1, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr && s.v == 3) warp_forward_kernel<32, 3, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr) warp_forward_kernel<32, 6, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1 && th <= 256) block_forward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1) block_forward_kernel<1, 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 2) block_forward_kernel<2, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  else block_forward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  return cudaGetLastError();
+}
+template <bool VEC, typename T>
+cudaError_t backward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
+  const int th = s.threads;
+  if (s.tpr == 8) warp_backward_kernel<8, true, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_backward_kernel<16, true, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr) warp_backward_kernel<32, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1) block_backward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 2) block_backward_kernel<2, block_rows<VEC, T>() / 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  else block_backward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch(const Norm &N, const Shape &s, bool backward, int blocks, cudaStream_t st) {
+  if (backward) return N.vec ? backward_typed<true, T>(N, s, blocks, st) : backward_typed<false, T>(N, s, blocks, st);
+  return N.vec ? forward_typed<true, T>(N, s, blocks, st) : forward_typed<false, T>(N, s, blocks, st);
+}
+cudaError_t launch_any(const Norm &N, const Shape &s, bool backward, int64_t dtype, int blocks, cudaStream_t st) {
+  if (dtype == NR_F32) return launch<float>(N, s, backward, blocks, st);
+  if (dtype == NR_F16) return launch<__half>(N, s, backward, blocks, st);
+  return launch<__nv_bfloat16>(N, s, backward, blocks, st);
+}
+constexpr int kLongParts = 32;
 
 }  // namespace
 
@@ -125,35 +758,59 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
   if (a->m == 0) return NR_OK;
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;
-  norm_forward_kernel<<<(unsigned)a->m, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-      rows_of(a), a->n, a->weight, a->bias, (int)a->w_dtype, (float)a->eps, a->y, a->y_ld, (int)a->dtype, a->mean,
-      a->rstd);
-  const cudaError_t e = cudaGetLastError();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const Norm N = norm_of(a, false);
+  const Shape sh = shape_of(a->n, N.vec, false);
+  cudaError_t e;
+  if (sh.threads) {
+    e = launch_any(N, sh, false, a->dtype, block_count(sh, a->m, false, nr_ops_sms(device)), s);
+  } else {
+    long_forward_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);
+    e = cudaGetLastError();
+  }
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }
 
-extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int) { return valid(a, true) ? 0 : -1; }
+extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int device) {
+  if (!valid(a, true)) return -1;
+  if (a->m == 0 || !a->dweight) return 0;
+  const Shape sh = shape_of(a->n, norm_of(a, true).vec, true);
+  const int64_t blocks = sh.threads ? block_count(sh, a->m, true, nr_ops_sms(device)) : kLongParts;
+  return round_up(blocks * 2 * a->n * 4, 256);
+}
 
-extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, void *, int64_t, void *stream) {
-  if (!valid(a, true)) return NR_ERR_INVALID_ARG;
+extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, void *ws, int64_t ws_bytes, void *stream) {
+  const int64_t need = nr_layer_norm_backward_workspace(a, device);
+  if (need < 0 || ws_bytes < need || (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))))
+    return NR_ERR_INVALID_ARG;
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
   if (a->m == 0) {
-    cudaError_t e = cudaSuccess;
     if (a->dweight) {
       e = cudaMemsetAsync(a->dweight, 0, (size_t)a->n * type_bytes(a->w_dtype), s);
       if (e == cudaSuccess) e = cudaMemsetAsync(a->dbias, 0, (size_t)a->n * type_bytes(a->w_dtype), s);
     }
     return e == cudaSuccess ? NR_OK : cuda_status(e);
   }
-  norm_dx_kernel<<<(unsigned)a->m, kThreads, 0, s>>>(a->dy, a->dy_ld, rows_of(a), a->n, a->weight, (int)a->w_dtype,
-                                                     a->mean, a->rstd, a->residual_grad, a->residual_grad_ld, a->dx,
-                                                     a->dx_ld, (int)a->dtype);
-  if (a->dweight)
-    norm_dparam_kernel<<<(unsigned)ceil_div(a->n, 32), 256, 0, s>>>(a->dy, a->dy_ld, rows_of(a), a->m, a->n, a->mean,
-                                                                    a->rstd, (int)a->dtype, a->dweight, a->dbias,
-                                                                    (int)a->w_dtype);
-  const cudaError_t e = cudaGetLastError();
+  Norm N = norm_of(a, true);
+  N.parts = a->dweight ? static_cast<float *>(ws) : nullptr;
+  const Shape sh = shape_of(a->n, N.vec, true);
+  int parts = kLongParts;
+  if (sh.threads) {
+    parts = block_count(sh, a->m, true, nr_ops_sms(device));
+    e = launch_any(N, sh, true, a->dtype, parts, s);
+  } else {
+    long_dx_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);
+    if (N.parts)
+      long_params_kernel<<<dim3((unsigned)ceil_div(a->n, 32), kLongParts), 256, 0, s>>>(N, (int)a->dtype);
+    e = cudaGetLastError();
+  }
+  if (e == cudaSuccess && N.parts) {
+    norm_params_kernel<<<(unsigned)ceil_div(2 * a->n, 32), 256, 0, s>>>(N.parts, parts, a->n, a->dweight, a->dbias,
+                                                                        (int)a->w_dtype);
+    e = cudaGetLastError();
+  }
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }

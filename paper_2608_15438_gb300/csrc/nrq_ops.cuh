@@ -25,6 +25,15 @@ __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2hal
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+template <typename T>
+struct TypeCode;
+template <>
+struct TypeCode<float> { static constexpr int code = NR_F32; };
+template <>
+struct TypeCode<__half> { static constexpr int code = NR_F16; };
+template <>
+struct TypeCode<__nv_bfloat16> { static constexpr int code = NR_BF16; };
+
 // one element of a runtime type
 __device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
   if (dtype == NR_F32) return static_cast<const float *>(p)[i];
@@ -36,6 +45,80 @@ __device__ __forceinline__ void store_any(void *p, int64_t i, int dtype, float v
   else if (dtype == NR_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
   else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
+
+// ------------------------------------------------------------ eight elements
+__device__ __forceinline__ uint32_t pack2(float a, float b, int dtype) {
+  if (dtype == NR_F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v, int dtype) {
+  if (dtype == NR_F16) return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&v));
+}
+
+// eight consecutive elements from (row pointer index) e on, `count` of them there
+__device__ __forceinline__ void load8(const void *p, int64_t e, int dtype, int vec, int count, float (&v)[8]) {
+  if (vec && count >= 8) {
+    if (dtype == NR_F32) {
+      const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e);
+      const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e + 4);
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+      const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + e);
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 f = unpack2(w[q], dtype);
+        v[2 * q] = f.x;
+        v[2 * q + 1] = f.y;
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = q < count ? load_any(p, e + q, dtype) : 0.0f;
+}
+__device__ __forceinline__ void store8(void *p, int64_t e, int dtype, int vec, int count, const float (&v)[8]) {
+  if (vec && count >= 8) {
+    if (dtype == NR_F32) {
+      float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(p) + e);
+      d[0] = make_float4(v[0], v[1], v[2], v[3]);
+      d[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + e) =
+          make_uint4(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype), pack2(v[4], v[5], dtype), pack2(v[6], v[7], dtype));
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (q < count) store_any(p, e + q, dtype, v[q]);
+}
+
+// ------------------------------------------------------------ pairs of fp32
+// one instruction for two values
+__device__ __forceinline__ unsigned long long bits2(float2 v) { return *reinterpret_cast<unsigned long long *>(&v); }
+__device__ __forceinline__ float2 from_bits2(unsigned long long v) { return *reinterpret_cast<float2 *>(&v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // ------------------------------------------------------------ activations
 // Phi(z) = erfc(-z / sqrt 2) / 2: no cancellation in the negative tail
@@ -78,9 +161,29 @@ __device__ __forceinline__ float held8_up(uint32_t s) {
 __device__ __forceinline__ float held8_down(uint32_t s) {
   return s == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float((s - 6u) << 23);
 }
-__device__ __forceinline__ int held8_code(float v, float up) {
-  const int q = __float2int_rn(v * up);  // NaN converts to 0
-  return max(-127, min(127, q));
+// The codes of four values in a word. Adding 1.5 2^23 rounds to a whole number,
+// ties to even, and leaves its two's complement in the low byte (a conversion
+// instruction runs at half the rate or less). Only the topmost scale (and 255)
+// can pass +-127.
+__device__ __forceinline__ uint32_t held8_codes(float2 a, float2 b, float up, uint32_t scale) {
+  if (scale >= 254u) {
+    a.x = fminf(fmaxf(a.x * up, -127.0f), 127.0f), a.y = fminf(fmaxf(a.y * up, -127.0f), 127.0f);
+    b.x = fminf(fmaxf(b.x * up, -127.0f), 127.0f), b.y = fminf(fmaxf(b.y * up, -127.0f), 127.0f);
+    up = 1.0f;
+  }
+  a = fma2(a, both(up), both(12582912.0f));
+  b = fma2(b, both(up), both(12582912.0f));
+  const uint32_t lo = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040);
+  const uint32_t hi = __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
+}
+// the four codes of a word as numbers: the byte + 128 under the exponent of 2^23
+__device__ __forceinline__ void held8_numbers(uint32_t codes, float2 &a, float2 &b) {
+  const uint32_t u = codes ^ 0x80808080u;
+  a.x = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)), a.y = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441));
+  b.x = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)), b.y = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443));
+  a = add2(a, both(-8388736.0f));
+  b = add2(b, both(-8388736.0f));
 }
 
 // ------------------------------------------------------------ host
@@ -88,6 +191,10 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 inline bool is_16bit(int64_t t) { return t == NR_F16 || t == NR_BF16; }
 inline size_t type_bytes(int64_t t) { return t == NR_F32 ? 4 : 2; }
+// whether eight columns of every row are a 16-byte access (two in fp32)
+inline bool vec_ok(const void *p, int64_t ld, int64_t dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (int64_t)type_bytes(dtype) % 16 == 0;
+}
 inline bool act_ok(int64_t a) { return a >= NR_ACT_NONE && a <= NR_ACT_SILU; }
 constexpr int64_t kOpsMaxRows = ((int64_t)1 << 31) - 1, kOpsMaxCols = ((int64_t)1 << 24) - 1;
 

@@ -45,25 +45,48 @@ class Checkpoint8:
         self.scales.record_stream(stream)
 
 
-def _matrix(t, name, dtypes, rows, cols, device):
-    """Checks a row-major matrix; returns its row pitch in elements."""
+_HALF = (torch.float16, torch.bfloat16)
+_FLOATS = tuple(_DT)
+_stream = torch._C._cuda_getCurrentRawStream  # the current stream of a device index, as an integer
+
+
+def _fail(t, name, dtypes, rows, cols, index):
+    """Says what is wrong with a matrix, in the order type, dtype, shape, device, strides."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-    sh = t.shape
-    if len(sh) != 2 or (rows is not None and sh[0] != rows) or (cols is not None and sh[1] != cols):
-        raise ValueError(f"{name}: shape {tuple(sh)}, expected ({'any' if rows is None else rows}, "
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({'any' if rows is None else rows}, "
                          f"{'any' if cols is None else cols})")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{name}: expected a tensor on {device or 'a CUDA device'}, got {t.device}")
-    ld, inner = t.stride()
-    if inner != 1 and sh[1] > 1:
-        raise ValueError(f"{name}: rows must be contiguous (stride(1) == 1)")
-    return ld
+    if not t.is_cuda or (index is not None and t.get_device() != index):
+        raise ValueError(f"{name}: expected a tensor on {'a CUDA device' if index is None else f'cuda:{index}'}, "
+                         f"got {t.device}")
+    if t.shape[1] < 1 or t.shape[1] >= 1 << 24:
+        raise ValueError(f"{name}: widths from 1 to 2^24 - 1 are supported, got {t.shape[1]}")
+    raise ValueError(f"{name}: rows must be contiguous (stride(1) == 1)")
 
 
-def _vector(t, name, dtypes, n, device):
+def _first(t, name, dtypes):
+    """Checks the row-major matrix that sets a call's sizes; (rows, columns, pitch, device index)."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.is_cuda and t.dim() == 2:
+        m, n = t.shape
+        ld, inner = t.stride()
+        if 0 < n < 16777216 and (inner == 1 or n == 1):
+            return m, n, ld, t.get_device()
+    _fail(t, name, dtypes, None, None, None)
+
+
+def _matrix(t, name, dtypes, rows, cols, index):
+    """Checks another matrix of the call; its row pitch in elements."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.get_device() == index and t.shape == (rows, cols):
+        ld, inner = t.stride()
+        if inner == 1 or cols == 1:
+            return ld
+    _fail(t, name, dtypes, rows, cols, index)
+
+
+def _vector(t, name, dtypes, n, index):
     if t is None:
         return 0
     if not isinstance(t, torch.Tensor):
@@ -72,20 +95,19 @@ def _vector(t, name, dtypes, n, device):
         raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
     if t.shape != (n,):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({n},)")
-    if t.device != device:
-        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
-    if n > 1 and t.stride(0) != 1:
+    if t.get_device() != index:
+        raise ValueError(f"{name}: expected a tensor on cuda:{index}, got {t.device}")
+    if n > 1 and t.stride() != (1,):
         raise ValueError(f"{name}: must be contiguous")
     return t.data_ptr()
 
 
-def _held(c, name, rows, cols, device, dtype):
-    if (rows is not None and c.shape[0] != rows) or (cols is not None and c.shape[1] != cols):
-        raise ValueError(f"{name}: shape {c.shape}, expected ({'any' if rows is None else rows}, "
-                         f"{'any' if cols is None else cols})")
-    if device is not None and c.device != device:
-        raise ValueError(f"{name}: expected a checkpoint on {device}, got {c.device}")
-    if dtype is not None and c.dtype != dtype:
+def _held(c, name, rows, cols, index, dtype):
+    if c.shape != (rows, cols):
+        raise ValueError(f"{name}: shape {c.shape}, expected ({rows}, {cols})")
+    if c.codes.get_device() != index:
+        raise ValueError(f"{name}: expected a checkpoint on cuda:{index}, got {c.device}")
+    if c.dtype is not dtype:
         raise ValueError(f"{name}: made from {c.dtype}, expected {dtype}")
 
 
@@ -94,16 +116,6 @@ def _act(name):
         return ACTIVATIONS[name]
     except (KeyError, TypeError):
         raise ValueError(f"act: {name!r}, expected one of {', '.join(ACTIVATIONS)}") from None
-
-
-def _widths(*dims):
-    for d in dims:
-        if d < 1 or d >= 1 << 24:
-            raise ValueError(f"widths from 1 to 2^24 - 1 are supported, got {d}")
-
-
-def _raw(device):
-    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _elsewhere(fn, stream, args, kw):
@@ -116,13 +128,14 @@ def _elsewhere(fn, stream, args, kw):
     return out
 
 
-def _run(call, packed, index, device, ws_bytes):
-    if ws_bytes < 0:
-        raise _nr.NRError(call, -1)
-    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=device) if ws_bytes else None
-    st = getattr(_nr.lib(), call)(packed, index, ws.data_ptr() if ws_bytes else 0, ws_bytes, _raw(device))
-    if st:
-        raise _nr.NRError(call, st)
+def _scratch(call, nbytes, device):
+    """Scratch of a call and its address."""
+    if nbytes <= 0:
+        if nbytes < 0:
+            raise _nr.NRError(call, -1)
+        return None, 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr()
 
 
 def _new_checkpoint(m, n, dtype, device):
@@ -135,12 +148,10 @@ def checkpoint8(x, stream=None) -> Checkpoint8:
     """x [m x n] (fp32, fp16 or bf16) held in 8 bits (nr_checkpoint8_write)."""
     if stream is not None:
         return _elsewhere(checkpoint8, stream, (x,), {})
-    ld = _matrix(x, "x", tuple(_DT), None, None, None)
-    m, n = x.shape
-    _widths(n)
+    m, n, ld, index = _first(x, "x", _FLOATS)
     c = _new_checkpoint(m, n, x.dtype, x.device)
     st = _nr.lib().nr_checkpoint8_write(x.data_ptr(), _DT[x.dtype], m, n, ld, c.codes.data_ptr(),
-                                        c.scales.data_ptr(), x.device.index, _raw(x.device))
+                                        c.scales.data_ptr(), index, _stream(index))
     if st:
         raise _nr.NRError("nr_checkpoint8_write", st)
     return c
@@ -155,8 +166,9 @@ def checkpoint8_read(c: Checkpoint8, act="none", stream=None):
     a = _act(act)
     m, n = c.shape
     y = torch.empty((m, n), dtype=c.dtype, device=c.device)
+    index = c.codes.get_device()
     st = _nr.lib().nr_checkpoint8_read(c.codes.data_ptr(), c.scales.data_ptr(), m, n, a, y.data_ptr(),
-                                       _DT[c.dtype], n, c.device.index, _raw(c.device))
+                                       _DT[c.dtype], n, index, _stream(index))
     if st:
         raise _nr.NRError("nr_checkpoint8_read", st)
     return y
@@ -173,37 +185,40 @@ def linear(x, w, bias=None, act="none", residual=None, save=None, out_dtype=None
     if stream is not None:
         return _elsewhere(linear, stream, (x, w, bias),
                           {"act": act, "residual": residual, "save": save, "out_dtype": out_dtype})
-    x_ld = _matrix(x, "x", (torch.float16, torch.bfloat16), None, None, None)
-    m, k = x.shape
+    m, k, x_ld, index = _first(x, "x", _HALF)
     dt, dev = x.dtype, x.device
-    w_ld = _matrix(w, "w", (dt,), None, k, dev)
-    n = w.shape[0]
-    _widths(k, n)
-    b = _vector(bias, "bias", (dt, torch.float32), n, dev)
+    n = w.shape[0] if isinstance(w, torch.Tensor) and w.dim() == 2 else None
+    w_ld = _matrix(w, "w", (dt,), n, k, index)
+    if not 0 < n < 16777216:
+        raise ValueError(f"w: widths from 1 to 2^24 - 1 are supported, got {n}")
+    b = _vector(bias, "bias", (dt, torch.float32), n, index)
     a = _act(act)
-    r = r_ld = 0
+    r = r_ld = z_ptr = z_scale = 0
     if residual is not None:
-        r_ld, r = _matrix(residual, "residual", (dt,), m, n, dev), residual.data_ptr()
+        r_ld, r = _matrix(residual, "residual", (dt,), m, n, index), residual.data_ptr()
     ydt = dt if out_dtype is None else out_dtype
     if ydt is not dt and ydt is not torch.float32:
         raise ValueError(f"out_dtype: {out_dtype}, expected {dt} or torch.float32")
     y = torch.empty((m, n), dtype=ydt, device=dev)
-    z = zp = zs = None
     if save == "z":
         z = torch.empty((m, n), dtype=dt, device=dev)
-        zp = z.data_ptr()
+        z_ptr = z.data_ptr()
     elif save == "z8":
         z = _new_checkpoint(m, n, dt, dev)
-        zp, zs = z.codes.data_ptr(), z.scales.data_ptr()
+        z_ptr, z_scale = z.codes.data_ptr(), z.scales.data_ptr()
     elif save is not None:
         raise ValueError(f"save: {save!r}, expected None, 'z' or 'z8'")
-    code = _DT[dt]
-    packed = _LINEAR.pack(m, k, n, code, _DT[ydt], code if bias is None else _DT[bias.dtype], a, x.data_ptr(),
-                          x_ld, 0, 0, w.data_ptr(), w_ld, b, r, r_ld, y.data_ptr(), n, zp or 0, n, zs or 0,
-                          0, 0, 0, 0, 0, 0)
-    _run("nr_linear_forward", packed, dev.index, dev,
-         _nr.lib().nr_linear_forward_workspace(packed, dev.index) if m else 0)
-    return y if z is None else (y, z)
+    if m:
+        code = _DT[dt]
+        packed = _LINEAR.pack(m, k, n, code, _DT[ydt], _DT[bias.dtype] if b else code, a, x.data_ptr(), x_ld, 0, 0,
+                              w.data_ptr(), w_ld, b, r, r_ld, y.data_ptr(), n, z_ptr, n, z_scale, 0, 0, 0, 0, 0, 0)
+        lib = _nr.lib()
+        nbytes = lib.nr_linear_forward_workspace(packed, index)
+        ws, ws_ptr = _scratch("nr_linear_forward", nbytes, dev)
+        st = lib.nr_linear_forward(packed, index, ws_ptr, nbytes, _stream(index))
+        if st:
+            raise _nr.NRError("nr_linear_forward", st)
+    return y if save is None else (y, z)
 
 
 def linear_backward(dy, x, w, z=None, act="none", x_act="none", bias_dtype=None, need=(True, True, True),
@@ -218,41 +233,52 @@ def linear_backward(dy, x, w, z=None, act="none", x_act="none", bias_dtype=None,
     if stream is not None:
         return _elsewhere(linear_backward, stream, (dy, x, w),
                           {"z": z, "act": act, "x_act": x_act, "bias_dtype": bias_dtype, "need": need})
-    w_ld = _matrix(w, "w", (torch.float16, torch.bfloat16), None, None, None)
-    n, k = w.shape
-    _widths(k, n)
+    n, k, w_ld, index = _first(w, "w", _HALF)
+    if not 0 < n < 16777216:
+        raise ValueError(f"w: widths from 1 to 2^24 - 1 are supported, got {n}")
     dt, dev = w.dtype, w.device
-    dy_ld = _matrix(dy, "dy", (dt, torch.float32), None, n, dev)
-    m = dy.shape[0]
-    xs = zp = z_ld = zs = 0
+    m = dy.shape[0] if isinstance(dy, torch.Tensor) and dy.dim() == 2 else None
+    dy_ld = _matrix(dy, "dy", (dt, torch.float32), m, n, index)
+    x_scale = x_ld = z_ptr = z_ld = z_scale = 0
     if isinstance(x, Checkpoint8):
-        _held(x, "x", m, k, dev, dt)
-        xp, x_ld, xs = x.codes.data_ptr(), 0, x.scales.data_ptr()
+        _held(x, "x", m, k, index, dt)
+        x_ptr, x_scale = x.codes.data_ptr(), x.scales.data_ptr()
     else:
-        x_ld, xp = _matrix(x, "x", (dt,), m, k, dev), x.data_ptr()
+        x_ld, x_ptr = _matrix(x, "x", (dt,), m, k, index), x.data_ptr()
         if x_act != "none":
             raise ValueError("x_act: only for an x held in 8 bits")
-    a, xa = _act(act), _act(x_act)
+    a = _act(act)
     if a:
         if z is None:
             raise ValueError("z: needed with an activation (linear's save='z' or 'z8')")
         if isinstance(z, Checkpoint8):
-            _held(z, "z", m, n, dev, dt)
-            zp, zs = z.codes.data_ptr(), z.scales.data_ptr()
+            _held(z, "z", m, n, index, dt)
+            z_ptr, z_scale = z.codes.data_ptr(), z.scales.data_ptr()
         else:
-            z_ld, zp = _matrix(z, "z", (dt,), m, n, dev), z.data_ptr()
+            z_ld, z_ptr = _matrix(z, "z", (dt,), m, n, index), z.data_ptr()
     bdt = torch.float32 if bias_dtype is None else bias_dtype
     if bdt is not dt and bdt is not torch.float32:
         raise ValueError(f"bias_dtype: {bias_dtype}, expected {dt} or torch.float32")
-    dx = torch.empty((m, k), dtype=dt, device=dev) if need[0] else None
-    dw = torch.empty((n, k), dtype=dt, device=dev) if need[1] else None
-    db = torch.empty(n, dtype=bdt, device=dev) if need[2] else None
-    packed = _LINEAR.pack(m, k, n, _DT[dt], _DT[dy.dtype], _DT[bdt], a, xp, x_ld, xs, xa, w.data_ptr(), w_ld,
-                          0, 0, 0, 0, 0, zp, z_ld, zs, dy.data_ptr(), dy_ld,
-                          dx.data_ptr() if need[0] else 0, k, dw.data_ptr() if need[1] else 0,
-                          db.data_ptr() if need[2] else 0)
-    _run("nr_linear_backward", packed, dev.index, dev,
-         _nr.lib().nr_linear_backward_workspace(packed, dev.index) if m else 0)
+    dx = dw = db = None
+    dx_ptr = dw_ptr = db_ptr = 0
+    if need[0]:
+        dx = torch.empty((m, k), dtype=dt, device=dev)
+        dx_ptr = dx.data_ptr()
+    if need[1]:
+        dw = torch.empty((n, k), dtype=dt, device=dev)
+        dw_ptr = dw.data_ptr()
+    if need[2]:
+        db = torch.empty(n, dtype=bdt, device=dev)
+        db_ptr = db.data_ptr()
+    packed = _LINEAR.pack(m, k, n, _DT[dt], _DT[dy.dtype], _DT[bdt], a, x_ptr, x_ld, x_scale, _act(x_act),
+                          w.data_ptr(), w_ld, 0, 0, 0, 0, 0, z_ptr, z_ld, z_scale, dy.data_ptr(), dy_ld, dx_ptr, k,
+                          dw_ptr, db_ptr)
+    lib = _nr.lib()
+    nbytes = lib.nr_linear_backward_workspace(packed, index)
+    ws, ws_ptr = _scratch("nr_linear_backward", nbytes, dev)
+    st = lib.nr_linear_backward(packed, index, ws_ptr, nbytes, _stream(index))
+    if st:
+        raise _nr.NRError("nr_linear_backward", st)
     return dx, dw, db
 
 
@@ -263,29 +289,32 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, stream=None):
     the same. save: returns (y, mean, rstd), mean and rstd [m] fp32."""
     if stream is not None:
         return _elsewhere(layer_norm, stream, (x, weight, bias), {"eps": eps, "save": save})
-    xs = x_ld = 0
+    x_scale = x_ld = 0
     if isinstance(x, Checkpoint8):
-        xp, xs = x.codes.data_ptr(), x.scales.data_ptr()
+        m, n = x.shape
+        index = x.codes.get_device()
+        x_ptr, x_scale = x.codes.data_ptr(), x.scales.data_ptr()
     else:
-        x_ld, xp = _matrix(x, "x", tuple(_DT), None, None, None), x.data_ptr()
-    m, n = x.shape
+        m, n, x_ld, index = _first(x, "x", _FLOATS)
+        x_ptr = x.data_ptr()
     dt, dev = x.dtype, x.device
-    _widths(n)
     wdt = weight.dtype if isinstance(weight, torch.Tensor) else bias.dtype if isinstance(bias, torch.Tensor) else dt
-    w = _vector(weight, "weight", (dt, torch.float32), n, dev)
-    b = _vector(bias, "bias", (wdt,) if weight is not None else (dt, torch.float32), n, dev)
+    w = _vector(weight, "weight", (dt, torch.float32), n, index)
+    b = _vector(bias, "bias", (wdt,) if w else (dt, torch.float32), n, index)
     if not eps > 0.0:
         raise ValueError(f"eps: {eps}, expected a positive number")
     y = torch.empty((m, n), dtype=dt, device=dev)
-    mean = rstd = None
+    mean_ptr = rstd_ptr = 0
     if save:
         mean = torch.empty(m, dtype=torch.float32, device=dev)
         rstd = torch.empty(m, dtype=torch.float32, device=dev)
-    packed = _NORM.pack(m, n, _DT[dt], _DT[wdt], eps, xp, x_ld, xs, w, b, y.data_ptr(), n,
-                        mean.data_ptr() if save else 0, rstd.data_ptr() if save else 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    st = _nr.lib().nr_layer_norm_forward(packed, dev.index, _raw(dev))
-    if st:
-        raise _nr.NRError("nr_layer_norm_forward", st)
+        mean_ptr, rstd_ptr = mean.data_ptr(), rstd.data_ptr()
+    packed = _NORM.pack(m, n, _DT[dt], _DT[wdt], eps, x_ptr, x_ld, x_scale, w, b, y.data_ptr(), n, mean_ptr, rstd_ptr,
+                        0, 0, 0, 0, 0, 0, 0, 0)
+    if m:
+        st = _nr.lib().nr_layer_norm_forward(packed, index, _stream(index))
+        if st:
+            raise _nr.NRError("nr_layer_norm_forward", st)
     return (y, mean, rstd) if save else y
 
 
@@ -298,34 +327,37 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual_grad=None, param_gra
     if stream is not None:
         return _elsewhere(layer_norm_backward, stream, (dy, x, weight, mean, rstd),
                           {"residual_grad": residual_grad, "param_grads": param_grads})
-    dy_ld = _matrix(dy, "dy", tuple(_DT), None, None, None)
-    m, n = dy.shape
+    m, n, dy_ld, index = _first(dy, "dy", _FLOATS)
     dt, dev = dy.dtype, dy.device
-    _widths(n)
-    xs = x_ld = r = r_ld = 0
+    x_scale = x_ld = r = r_ld = 0
     if isinstance(x, Checkpoint8):
-        _held(x, "x", m, n, dev, dt)
-        xp, xs = x.codes.data_ptr(), x.scales.data_ptr()
+        _held(x, "x", m, n, index, dt)
+        x_ptr, x_scale = x.codes.data_ptr(), x.scales.data_ptr()
     else:
-        x_ld, xp = _matrix(x, "x", (dt,), m, n, dev), x.data_ptr()
-    w = _vector(weight, "weight", (dt, torch.float32), n, dev)
-    mp = _vector(mean, "mean", (torch.float32,), m, dev)
-    rp = _vector(rstd, "rstd", (torch.float32,), m, dev)
+        x_ld, x_ptr = _matrix(x, "x", (dt,), m, n, index), x.data_ptr()
+    w = _vector(weight, "weight", (dt, torch.float32), n, index)
     if mean is None or rstd is None:
         raise ValueError("mean, rstd: needed (layer_norm's save=True)")
+    mean_ptr = _vector(mean, "mean", (torch.float32,), m, index)
+    rstd_ptr = _vector(rstd, "rstd", (torch.float32,), m, index)
     if residual_grad is not None:
-        r_ld, r = _matrix(residual_grad, "residual_grad", (dt,), m, n, dev), residual_grad.data_ptr()
+        r_ld, r = _matrix(residual_grad, "residual_grad", (dt,), m, n, index), residual_grad.data_ptr()
     wdt = torch.float32 if weight is None else weight.dtype
     dx = torch.empty((m, n), dtype=dt, device=dev)
     dw = db = None
+    dw_ptr = db_ptr = 0
     if param_grads:
         dw = torch.empty(n, dtype=wdt, device=dev)
         db = torch.empty(n, dtype=wdt, device=dev)
-    packed = _NORM.pack(m, n, _DT[dt], _DT[wdt], 0.0, xp, x_ld, xs, w, 0, 0, 0, mp, rp, dy.data_ptr(), dy_ld, r,
-                        r_ld, dx.data_ptr(), n, dw.data_ptr() if param_grads else 0,
-                        db.data_ptr() if param_grads else 0)
-    _run("nr_layer_norm_backward", packed, dev.index, dev,
-         _nr.lib().nr_layer_norm_backward_workspace(packed, dev.index) if m else 0)
+        dw_ptr, db_ptr = dw.data_ptr(), db.data_ptr()
+    packed = _NORM.pack(m, n, _DT[dt], _DT[wdt], 0.0, x_ptr, x_ld, x_scale, w, 0, 0, 0, mean_ptr, rstd_ptr,
+                        dy.data_ptr(), dy_ld, r, r_ld, dx.data_ptr(), n, dw_ptr, db_ptr)
+    lib = _nr.lib()
+    nbytes = lib.nr_layer_norm_backward_workspace(packed, index)
+    ws, ws_ptr = _scratch("nr_layer_norm_backward", nbytes, dev)
+    st = lib.nr_layer_norm_backward(packed, index, ws_ptr, nbytes, _stream(index))
+    if st:
+        raise _nr.NRError("nr_layer_norm_backward", st)
     return dx, dw, db
 
 
