@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads)
       for (int q = 0; q < 4; ++q) p[q] = mul2(p[q], both(down));
       if (act != NR_ACT_NONE) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) p[q] = make_float2(act_value(p[q].x, act), act_value(p[q].y, act));
+        for (int q = 0; q < 4; ++q) p[q] = act_value2(p[q], act);
       }
       if (TypeCode<T>::code == NR_F16 && s[u] >= 143u) {  // 64 x 2^10 stands for up to 65504: keep it finite; NaN stays
 #pragma unroll

@@ -54,58 +54,141 @@ struct Epilogue {
   uint8_t *z_scale;
   int64_t n;
   int dtype, y_dtype;
-  int y_vec, z_vec, residual_vec;  // eight columns a 16-byte access (32 bytes in fp32)
+  int y_vec, z_vec, residual_vec, bias_vec;  // eight columns a 16-byte access (32 bytes in fp32)
 };
 
-// Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'). The four
-// threads of a group of 32 columns call it together (lanes 4 a .. 4 a + 3 of a
-// warp, in column order), row_ok false for rows past the end.
-__device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int64_t j, bool row_ok, float (&v)[8],
-                                        const float (&bias)[8]) {
-  const int count = row_ok ? (int)min((int64_t)8, E.n - j) : 0;  // may be negative
+// z of eight columns in 8 bits: the four threads of a group of 32 columns together
+// (lanes 4 a .. 4 a + 3 of a warp, in column order); count: columns there
+__device__ __forceinline__ void hold8(const Epilogue &E, int64_t i, int j, bool row_ok, int count, const float2 (&v)[4]) {
+  float2 u[4];
+  uint32_t top = 0;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] += bias[q];
+  for (int q = 0; q < 4; ++q) {
+    u[q] = make_float2(2 * q < count ? v[q].x : 0.0f, 2 * q + 1 < count ? v[q].y : 0.0f);
+    top = max(top, max(__float_as_uint(u[q].x) & 0x7fffffffu, __float_as_uint(u[q].y) & 0x7fffffffu));
+  }
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t sc = held8_scale(top);
+  const float up = held8_up(sc);
+  const int groups = ((int)E.n + kOpsGroup - 1) / kOpsGroup;
+  if (row_ok && j < groups * kOpsGroup) {
+    *reinterpret_cast<uint2 *>(static_cast<int8_t *>(E.z) + i * groups * kOpsGroup + j) =
+        make_uint2(held8_codes(u[0], u[1], up, sc), held8_codes(u[2], u[3], up, sc));
+    if ((j & (kOpsGroup - 1)) == 0) E.z_scale[i * groups + (j >> 5)] = (uint8_t)sc;
+  }
+}
+__device__ __forceinline__ void add_raw(float2 (&v)[4], const uint4 &r, int dtype) {
+  v[0] = add2(v[0], unpack2(r.x, dtype)), v[1] = add2(v[1], unpack2(r.y, dtype));
+  v[2] = add2(v[2], unpack2(r.z, dtype)), v[3] = add2(v[3], unpack2(r.w, dtype));
+}
+__device__ __forceinline__ uint4 pack8(const float2 (&v)[4], int dtype) {
+  return make_uint4(pack2(v[0].x, v[0].y, dtype), pack2(v[1].x, v[1].y, dtype), pack2(v[2].x, v[2].y, dtype),
+                    pack2(v[3].x, v[3].y, dtype));
+}
+
+// Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'), row_ok
+// false for rows past the end; called as hold8 is.
+__device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, bool row_ok, float2 (&v)[4],
+                                        const float2 (&bias)[4]) {
+  const int count = row_ok ? min(8, (int)E.n - j) : 0;  // may be negative
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = add2(v[q], bias[q]);
   if (E.z) {
     if (E.z_scale) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (q < count) top = max(top, __float_as_uint(v[q]) & 0x7fffffffu);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const uint32_t sc = held8_scale(top);
-      const float up = held8_up(sc);
-      const int64_t groups = (E.n + kOpsGroup - 1) / kOpsGroup;
-      if (row_ok && j < groups * kOpsGroup) {
-        float u[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) u[q] = q < count ? v[q] : 0.0f;
-        *reinterpret_cast<uint2 *>(static_cast<int8_t *>(E.z) + i * groups * kOpsGroup + j) =
-            make_uint2(held8_codes(make_float2(u[0], u[1]), make_float2(u[2], u[3]), up, sc),
-                       held8_codes(make_float2(u[4], u[5]), make_float2(u[6], u[7]), up, sc));
-        if ((j & (kOpsGroup - 1)) == 0) E.z_scale[i * groups + (j >> 5)] = (uint8_t)sc;
-      }
+      hold8(E, i, j, row_ok, count, v);
     } else if (count > 0) {
-      store8(E.z, i * E.z_ld + j, E.dtype, E.z_vec, count, v);
+      const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
+      store8(E.z, i * E.z_ld + j, E.dtype, E.z_vec, count, o);
     }
   }
   if (count <= 0) return;
   if (E.act != NR_ACT_NONE) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = act_value(v[q], E.act);
+    for (int q = 0; q < 4; ++q) v[q] = act_value2(v[q], E.act);
   }
   if (E.residual) {
     float r[8];
     load8(E.residual, i * E.residual_ld + j, E.dtype, E.residual_vec, count, r);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] += r[q];
+    for (int q = 0; q < 4; ++q) v[q] = add2(v[q], make_float2(r[2 * q], r[2 * q + 1]));
   }
-  store8(E.y, i * E.y_ld + j, E.y_dtype, E.y_vec, count, v);
+  const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
+  store8(E.y, i * E.y_ld + j, E.y_dtype, E.y_vec, count, o);
 }
 
-__device__ __forceinline__ void bias8(const Epilogue &E, int64_t j, float (&b)[8]) {
+__device__ __forceinline__ void bias8(const Epilogue &E, int j, float2 (&b)[4]) {
+  if (E.bias && E.bias_vec && j + 8 <= (int)E.n) {
+    float o[8];
+    load8(E.bias, j, E.bias_dtype, 1, 8, o);
 #pragma unroll
-  for (int q = 0; q < 8; ++q) b[q] = E.bias && j + q < E.n ? load_any(E.bias, j + q, E.bias_dtype) : 0.0f;
+    for (int q = 0; q < 4; ++q) b[q] = make_float2(o[2 * q], o[2 * q + 1]);
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    b[q].x = E.bias && j + 2 * q < (int)E.n ? load_any(E.bias, j + 2 * q, E.bias_dtype) : 0.0f;
+    b[q].y = E.bias && j + 2 * q + 1 < (int)E.n ? load_any(E.bias, j + 2 * q + 1, E.bias_dtype) : 0.0f;
+  }
+}
+
+// A warp's 32 x 32 block of sums: from tensor memory (a thread a row) through
+// shared memory to eight columns of four rows a thread, so that the global
+// accesses run along rows. 16-byte piece q of row r lies at piece q ^ (r % 8): both
+// the rows' threads and the eight columns' touch all banks.
+__device__ __forceinline__ void stage_write(float *stage, int lane, const uint32_t (&v)[32]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    *reinterpret_cast<uint4 *>(stage + lane * 32 + ((q ^ (lane & 7)) << 2)) =
+        make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+}
+__device__ __forceinline__ void stage_read(const float *stage, int lane, int u, float2 (&v)[4]) {
+  const int seg = lane & 3, r8 = lane >> 2;
+  const float4 lo = *reinterpret_cast<const float4 *>(stage + (u * 8 + r8) * 32 + (((2 * seg) ^ r8) << 2));
+  const float4 hi = *reinterpret_cast<const float4 *>(stage + (u * 8 + r8) * 32 + (((2 * seg + 1) ^ r8) << 2));
+  v[0] = make_float2(lo.x, lo.y), v[1] = make_float2(lo.z, lo.w);
+  v[2] = make_float2(hi.x, hi.y), v[3] = make_float2(hi.z, hi.w);
+}
+
+// A whole block (32 rows and columns there, every matrix in vectors, y 16-bit) from
+// row i, column j of the thread's eight: no bounds, one test a step for all rows.
+__device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j, const float *stage, int lane,
+                                             const float2 (&b)[4], const uint4 (&res)[4]) {
+  float2 v[4][4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    stage_read(stage, lane, u, v[u]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[u][q] = add2(v[u][q], b[q]);
+  }
+  if (E.z) {
+    if (E.z_scale) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) hold8(E, i + 8 * u, j, true, 8, v[u]);
+    } else {
+      uint16_t *z = static_cast<uint16_t *>(E.z) + i * E.z_ld + j;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4 *>(z + 8 * u * E.z_ld) = pack8(v[u], E.dtype);
+    }
+  }
+#define NR_BLOCK_ACT(A)                                  \
+  _Pragma("unroll") for (int u = 0; u < 4; ++u)          \
+  _Pragma("unroll") for (int q = 0; q < 4; ++q) v[u][q] = act_value2(v[u][q], A);
+  if (E.act == NR_ACT_GELU) {
+    NR_BLOCK_ACT(NR_ACT_GELU)
+  } else if (E.act == NR_ACT_SILU) {
+    NR_BLOCK_ACT(NR_ACT_SILU)
+  } else if (E.act == NR_ACT_RELU) {
+    NR_BLOCK_ACT(NR_ACT_RELU)
+  }
+#undef NR_BLOCK_ACT
+  if (E.residual) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add_raw(v[u], res[u], E.dtype);
+  }
+  uint16_t *y = static_cast<uint16_t *>(E.y) + i * E.y_ld + j;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4 *>(y + 8 * u * E.y_ld) = pack8(v[u], E.dtype);
 }
 
 // ------------------------------------------------------------ products on tensor cores
@@ -116,8 +199,7 @@ constexpr int kWarpProd = 0, kWarpMma = 1, kWarpEpi = 2;
 constexpr int kThreads = 32 * (kWarpEpi + kEpiWarps);
 constexpr int kStagesMax = 8;
 constexpr uint32_t kABytes = kRows * kSlice * 2;
-constexpr int kPitch = 36;            // floats a staged row: 16-byte accesses of 8 lanes hit all banks
-constexpr uint32_t kStaging = 32 * kPitch * 4;  // a warp's 32 x 32 block
+constexpr uint32_t kStaging = 32 * 32 * 4;  // a warp's 32 x 32 block of sums
 constexpr int64_t kWaitNs = 1000000000;
 
 struct Bars {
@@ -191,16 +273,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (warp == kWarpProd) {
     if (lane == 0) {
-      uint32_t g = 0;
+      uint32_t st = 0, phase = 1;  // the stage's wait parity: free at first
       bool ok = true;
       for (int item = first; item < items && ok; item += step) {
         int tm, tn, part;
         item_of(P, item, tm, tn, part);
         const int i0 = (tm * CG + (int)rank) * kRows, j0 = tn * P.nt + (int)rank * nb;
         const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
-        for (int s = s0; s < s1; ++s, ++g) {
-          const uint32_t st = g % nstages;
-          if (!tc::bar_wait(tc::smem_u32(&B.empty[st]), ((g / nstages) & 1u) ^ 1u, abort, P.wait_ns)) {
+        for (int s = s0; s < s1; ++s) {
+          if (!tc::bar_wait(tc::smem_u32(&B.empty[st]), phase, abort, P.wait_ns)) {
             ok = false;
             break;
           }
@@ -220,36 +301,47 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
           } else {
             tc::load_2d<CG>(sb, &mb, t0, j0, bar);
           }
+          if (++st == nstages) st = 0, phase ^= 1u;
         }
       }
     }
     __syncwarp();
   } else if (warp == kWarpMma) {
     if (lane == 0 && rank == 0) {
-      uint32_t g = 0, it = 0;
+      uint32_t it = 0, st = 0, phase = 0;
       bool ok = true;
       // 16 values of t: 32 bytes along 128-byte rows, or 16 rows of 128 bytes
-      const uint32_t step_a = P.a_outer ? 2048u : 32u, step_b = P.b_outer ? 2048u : 32u;
+      // (descriptors count in 16 bytes)
+      const uint64_t step_a = P.a_outer ? 128u : 2u, step_b = P.b_outer ? 128u : 2u, step_st = stage_bytes >> 4;
+      const uint64_t da0 = tc::desc128(base, 8192u), db0 = tc::desc128(base + kABytes, 8192u);
+      uint64_t da = da0, db = db0;
+      // The next stage's barrier is awaited in the middle of a stage's MMAs: the
+      // tensor pipe holds about two MMAs, which cover the wait there but not
+      // one between stages (720 against 512 cycles a stage of 256 x 256).
       for (int item = first; item < items && ok; item += step, ++it) {
         int tm, tn, part;
         item_of(P, item, tm, tn, part);
         const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
         const uint32_t a = it & 1u, d = tmem + a * (uint32_t)P.nt;
-        if (!tc::bar_wait(tc::smem_u32(&B.accempty[a]), ((it >> 1) & 1u) ^ 1u, abort, P.wait_ns)) break;
+        if (!tc::bar_wait(tc::smem_u32(&B.accempty[a]), ((it >> 1) & 1u) ^ 1u, abort, P.wait_ns) ||
+            !tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, P.wait_ns))
+          break;
         tc::fence_after();
-        for (int s = s0; s < s1; ++s, ++g) {
-          const uint32_t st = g % nstages;
-          if (!tc::bar_wait(tc::smem_u32(&B.full[st]), (g / nstages) & 1u, abort, P.wait_ns)) {
-            ok = false;
-            break;
-          }
+        for (int left = s1 - s0; left > 0; --left) {
+          const uint32_t bar = tc::smem_u32(&B.empty[st]);
+          const bool wrap = st + 1 == nstages;
+          tc::mma<CG>(d, da, db, P.idesc, left != s1 - s0);
+          tc::mma<CG>(d, da + step_a, db + step_b, P.idesc, 1u);
+          st = wrap ? 0u : st + 1;
+          phase ^= wrap ? 1u : 0u;
+          ok = left == 1 || tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, P.wait_ns);
           tc::fence_after();
-          const uint32_t sa = base + st * stage_bytes, sb = sa + kABytes;
-#pragma unroll
-          for (uint32_t k = 0; k < kSlice / 16; ++k)
-            tc::mma<CG>(d, tc::desc128(sa + k * step_a, 8192u), tc::desc128(sb + k * step_b, 8192u), P.idesc,
-                        (s > s0 || k > 0) ? 1u : 0u);
-          tc::commit<CG>(tc::smem_u32(&B.empty[st]));
+          tc::mma<CG>(d, da + 2 * step_a, db + 2 * step_b, P.idesc, 1u);
+          tc::mma<CG>(d, da + 3 * step_a, db + 3 * step_b, P.idesc, 1u);
+          tc::commit<CG>(bar);
+          if (!ok) break;
+          da = wrap ? da0 : da + step_st;
+          db = wrap ? db0 : db + step_st;
         }
         if (ok) tc::commit<CG>(tc::smem_u32(&B.accfull[a]));
       }
@@ -265,52 +357,65 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     const int lg = warp & 3;  // the quarter of the lanes this warp may read
     const uint32_t lane_base = (uint32_t)(lg * 32) << 16;
     float *stage = reinterpret_cast<float *>(smem + o_staging + (uint32_t)ew * kStaging);
-    const int seg = lane & 3, r8 = lane >> 2;
+    const int seg = lane & 3, r8 = lane >> 2, n = (int)E.n;
+    const bool vectors = E.y_vec && E.y_dtype != NR_F32 && (!E.z || E.z_scale || E.z_vec) && (!E.residual || E.residual_vec) &&
+                         !P.partial;
+    const uint32_t accempty0 = tc::map_rank(tc::smem_u32(&B.accempty[0]), 0);
     uint32_t it = 0;
     for (int item = first; item < items; item += step, ++it) {
       int tm, tn, part;
       item_of(P, item, tm, tn, part);
       const uint32_t a = it & 1u;
+      const int64_t i0 = ((int64_t)tm * CG + rank) * kRows + lg * 32;
+      // the two warps of a lane quarter take its chunks of 32 columns in turn
+      const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < P.rows ? min(n, (tn + 1) * P.nt) : 0;
       if (__all_sync(0xffffffffu, tc::bar_wait(tc::smem_u32(&B.accfull[a]), (it >> 1) & 1u, abort, P.wait_ns)) == 0) break;
       tc::fence_after();
-      const int64_t i0 = ((int64_t)tm * CG + rank) * kRows + lg * 32;
-      for (int c = ew >> 2; c * 32 < P.nt; c += 2) {  // the two warps of a lane quarter take chunks in turn
-        const int64_t j = (int64_t)tn * P.nt + c * 32 + seg * 8;
-        const bool live = (int64_t)tn * P.nt + c * 32 < E.n && i0 < P.rows;
-        if (!live) continue;  // the whole warp
-        __syncwarp();  // the block's previous readers are done
+      const uint32_t acc = tmem + lane_base + a * (uint32_t)P.nt - (uint32_t)(tn * P.nt);
+      for (int c = c0; c < c1; c += 64) {
         uint32_t v[32];
-        tc::ld32(tmem + lane_base + a * (uint32_t)P.nt + (uint32_t)c * 32u, v);
+        __syncwarp();  // the block's previous readers are done
+        tc::ld32(acc + (uint32_t)c, v);
+        const int j = c + seg * 8;
+        const bool whole = vectors && c + 32 <= n && i0 + 32 <= P.rows;
+        // meanwhile, what the read-back needs
+        float2 b[4];
+        uint4 res[4];
+        if (E.bias) {
+          bias8(E, j, b);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) b[q] = both(0.0f);
+        }
+        if (E.residual && whole) {
+          const uint16_t *p = static_cast<const uint16_t *>(E.residual) + (i0 + r8) * E.residual_ld + j;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) res[u] = __ldg(reinterpret_cast<const uint4 *>(p + 8 * u * E.residual_ld));
+        }
         tc::wait_ld();
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          *reinterpret_cast<uint4 *>(stage + lane * kPitch + 4 * q) =
-              make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        stage_write(stage, lane, v);
         __syncwarp();
-        float b[8];
-        if (!P.partial) bias8(E, j, b);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = u * 8 + r8;
-          const float4 lo = *reinterpret_cast<const float4 *>(stage + r * kPitch + seg * 8);
-          const float4 hi = *reinterpret_cast<const float4 *>(stage + r * kPitch + seg * 8 + 4);
-          float s[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-          const int64_t i = i0 + r;
-          if (P.partial) {
-            if (i < P.rows && j < E.n)  // the pitch is a multiple of 8
-              store8(E.y, ((int64_t)part * P.rows + i) * E.y_ld + j, NR_F32, 1, 8, s);
-          } else {
-            finish8(E, i, j, i < P.rows, s, b);
+        if (whole) {
+          finish_block(E, i0 + r8, j, stage, lane, b, res);
+        } else {
+#pragma unroll 1
+          for (int u = 0; u < 4; ++u) {
+            float2 s[4];
+            stage_read(stage, lane, u, s);
+            const int64_t i = i0 + u * 8 + r8;
+            if (!P.partial) {
+              finish8(E, i, j, i < P.rows, s, b);
+            } else if (i < P.rows && j < n) {  // the pitch is a multiple of 8
+              float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(E.y) + ((int64_t)part * P.rows + i) * E.y_ld + j);
+              p[0] = make_float4(s[0].x, s[0].y, s[1].x, s[1].y);
+              p[1] = make_float4(s[2].x, s[2].y, s[3].x, s[3].y);
+            }
           }
         }
       }
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) {
-        uint32_t bar = tc::smem_u32(&B.accempty[a]);
-        bar = tc::map_rank(bar, 0);
-        tc::bar_arrive_cluster(bar);
-      }
+      if (lane == 0) tc::bar_arrive_cluster(accempty0 + a * 8u);
     }
   }
   tc::fence_before();
@@ -338,17 +443,18 @@ __global__ void __launch_bounds__(256)
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t i = e / segs, j = (e - i * segs) * 8;
   const bool row_ok = i < rows;
-  float v[8] = {}, b[8];
+  float2 v[4] = {}, b[4];
   if (row_ok && j < E.n) {
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
-      float p[8];
-      load8(parts, ((int64_t)s * rows + i) * part_ld + j, NR_F32, 1, 8, p);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] += p[q];
+      const float4 *p = reinterpret_cast<const float4 *>(parts + ((int64_t)s * rows + i) * part_ld + j);
+      const float4 lo = __ldg(p), hi = __ldg(p + 1);
+      v[0] = add2(v[0], make_float2(lo.x, lo.y)), v[1] = add2(v[1], make_float2(lo.z, lo.w));
+      v[2] = add2(v[2], make_float2(hi.x, hi.y)), v[3] = add2(v[3], make_float2(hi.z, hi.w));
     }
   }
-  bias8(E, j, b);
-  finish8(E, i, j, row_ok, v, b);
+  bias8(E, (int)j, b);
+  finish8(E, i, (int)j, row_ok, v, b);
 }
 
 // ------------------------------------------------------------ few rows, on CUDA cores
@@ -477,7 +583,11 @@ __global__ void __launch_bounds__(256)
         float s[8];
         saved8(z, i, j, dtype, count, s);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= act_slope(s[q], act);
+        for (int q = 0; q < 8; q += 2) {
+          const float2 d = mul2(make_float2(v[q], v[q + 1]), act_slope2(make_float2(s[q], s[q + 1]), act));
+          v[q] = d.x;
+          v[q + 1] = d.y;
+        }
       }
       if (dz) store8(dz, i * dz_ld + j, dtype, 1, 8, v);  // the pitch is a multiple of 8
 #pragma unroll
@@ -844,6 +954,7 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
   E.y_vec = vec_ok(a->y, a->y_ld, a->y_dtype);
   E.z_vec = vec_ok(a->z, a->z_ld, a->dtype);
   E.residual_vec = vec_ok(a->residual, a->residual_ld, a->dtype);
+  E.bias_vec = vec_ok(a->bias, 8, a->bias_dtype);
   if (f.few) {
     if (a->z_scale) {
       E.z = at(ws, f.z_at);
