@@ -208,16 +208,35 @@ struct Bars {
   int abort;
 };
 
+// One product, and how it is cut.
 struct Product {
   int64_t rows;          // of C
   int tiles_m, tiles_n;  // tiles of 128 CG rows, of nt columns
-  int nt, stages;
+  int nt;
   int slices, splits;    // of 64 values of t; parts of them
   int a_outer, b_outer;  // the operand's own index is the contiguous one
   uint32_t idesc;
-  int partial;           // part s's sums go to y + s rows y_ld, nothing else
+  float *parts;          // splits > 1: part s's sums go to parts + s rows parts_ld
+  int64_t parts_ld;
+  Epilogue E;
+};
+
+// A launch: one product, or two that share the GPU (the second's tiles fill what the
+// first's leave idle).
+struct Job {
+  Product p[2];
+  int items0, items;     // work items of the first, of both
+  int nt, stages;        // the wider tile's columns
+  uint32_t stage_bytes;
+  int *flag;
   int64_t wait_ns;
 };
+
+// Items go to the CTAs (pairs) in turns that run forwards and backwards, so that a
+// last, short turn falls to those that had the shorter items.
+__device__ __forceinline__ int item_at(int turn, int slot, int slots) {
+  return turn * slots + ((turn & 1) ? slots - 1 - slot : slot);
+}
 
 // an item's tile and part. Tiles run down bands of 8 tile rows, so that the
 // tiles in flight share their slices of A and B in L2.
@@ -232,27 +251,30 @@ __device__ __forceinline__ void item_of(const Product &P, int item, int &tm, int
   tm = band * kBand + in - tn * height;
 }
 
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+__device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+
 template <int CG>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const Product P,
-                   const Epilogue E, int *flag) {
+    product_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap mb0,
+                   const __grid_constant__ CUtensorMap ma1, const __grid_constant__ CUtensorMap mb1,
+                   const __grid_constant__ Job J) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char *smem = smem_raw + (base - tc::smem_u32(smem_raw));
-  const int nb = P.nt / CG;  // rows of B this CTA holds
-  const uint32_t stage_bytes = kABytes + (uint32_t)nb * kSlice * 2;
-  const uint32_t o_staging = (uint32_t)P.stages * stage_bytes, o_bars = o_staging + kEpiWarps * kStaging;
+  const uint32_t o_staging = (uint32_t)J.stages * J.stage_bytes, o_bars = o_staging + kEpiWarps * kStaging;
   Bars &B = *reinterpret_cast<Bars *>(smem + o_bars);
   volatile int *abort = &B.abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0u;
-  const int items = P.tiles_m * P.tiles_n * P.splits, first = blockIdx.x / CG, step = gridDim.x / CG;
+  const int slot = blockIdx.x / CG, slots = gridDim.x / CG;
+  const int64_t limit = J.wait_ns;
   uint32_t cols = 32;
-  while (cols < 2u * (uint32_t)P.nt) cols <<= 1;
+  while (cols < 2u * (uint32_t)J.nt) cols <<= 1;
 
   if (warp == kWarpMma) tc::alloc<CG>(tc::smem_u32(&B.tmem_slot), cols);
   if (tid == 0) {
-    for (int i = 0; i < P.stages; ++i) {
+    for (int i = 0; i < J.stages; ++i) {
       tc::bar_init(tc::smem_u32(&B.full[i]), 1);
       tc::bar_init(tc::smem_u32(&B.empty[i]), 1);
     }
@@ -269,82 +291,106 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   if (CG == 2) tc::cluster_sync();
   tc::fence_after();
   const uint32_t tmem = B.tmem_slot;
-  const uint32_t nstages = (uint32_t)P.stages;
+  const uint32_t nstages = (uint32_t)J.stages;
+  grid_wait();  // what the previous launch of this call wrote is there
+  grid_launch();
 
+  // The roles below take the first product's items, then the second's, in code of
+  // their own: a product picked by index would keep its constants out of the
+  // uniform registers that copies and MMAs are issued from (up to a third slower).
   if (warp == kWarpProd) {
     if (lane == 0) {
       uint32_t st = 0, phase = 1;  // the stage's wait parity: free at first
+      int turn = 0;
       bool ok = true;
-      for (int item = first; item < items && ok; item += step) {
-        int tm, tn, part;
-        item_of(P, item, tm, tn, part);
-        const int i0 = (tm * CG + (int)rank) * kRows, j0 = tn * P.nt + (int)rank * nb;
-        const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
-        for (int s = s0; s < s1; ++s) {
-          if (!tc::bar_wait(tc::smem_u32(&B.empty[st]), phase, abort, P.wait_ns)) {
-            ok = false;
-            break;
+      auto produce = [&](const Product &P, const CUtensorMap *ma, const CUtensorMap *mb, int from, int to) {
+        const int nb = P.nt / CG;  // rows of B this CTA holds
+        const uint32_t bytes = kABytes + (uint32_t)nb * kSlice * 2;
+        for (; ok; ++turn) {
+          const int item = item_at(turn, slot, slots);
+          if (item >= to) break;
+          int tm, tn, part;
+          item_of(P, item - from, tm, tn, part);
+          const int i0 = (tm * CG + (int)rank) * kRows, j0 = tn * P.nt + (int)rank * nb;
+          const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
+          for (int s = s0; s < s1; ++s) {
+            if (!tc::bar_wait(tc::smem_u32(&B.empty[st]), phase, abort, limit)) {
+              ok = false;
+              break;
+            }
+            // the pair's bytes are counted on the first CTA's barrier
+            uint32_t bar = tc::smem_u32(&B.full[st]);
+            if (rank == 0) tc::bar_expect(bar, CG * bytes);
+            if (CG == 2) bar = tc::map_rank(bar, 0);
+            const uint32_t sa = base + st * J.stage_bytes, sb = sa + kABytes;
+            const int t0 = s * kSlice;
+            if (P.a_outer) {
+              for (int q = 0; q < kRows / 64; ++q) tc::load_2d<CG>(sa + (uint32_t)q * 8192u, ma, i0 + q * 64, t0, bar);
+            } else {
+              tc::load_2d<CG>(sa, ma, t0, i0, bar);
+            }
+            if (P.b_outer) {
+              for (int q = 0; q < nb / 64; ++q) tc::load_2d<CG>(sb + (uint32_t)q * 8192u, mb, j0 + q * 64, t0, bar);
+            } else {
+              tc::load_2d<CG>(sb, mb, t0, j0, bar);
+            }
+            if (++st == nstages) st = 0, phase ^= 1u;
           }
-          // the pair's bytes are counted on the first CTA's barrier
-          uint32_t bar = tc::smem_u32(&B.full[st]);
-          if (rank == 0) tc::bar_expect(bar, CG * stage_bytes);
-          if (CG == 2) bar = tc::map_rank(bar, 0);
-          const uint32_t sa = base + st * stage_bytes, sb = sa + kABytes;
-          const int t0 = s * kSlice;
-          if (P.a_outer) {
-            for (int q = 0; q < kRows / 64; ++q) tc::load_2d<CG>(sa + (uint32_t)q * 8192u, &ma, i0 + q * 64, t0, bar);
-          } else {
-            tc::load_2d<CG>(sa, &ma, t0, i0, bar);
-          }
-          if (P.b_outer) {
-            for (int q = 0; q < nb / 64; ++q) tc::load_2d<CG>(sb + (uint32_t)q * 8192u, &mb, j0 + q * 64, t0, bar);
-          } else {
-            tc::load_2d<CG>(sb, &mb, t0, j0, bar);
-          }
-          if (++st == nstages) st = 0, phase ^= 1u;
         }
-      }
+      };
+      produce(J.p[0], &ma0, &mb0, 0, J.items0);
+      produce(J.p[1], &ma1, &mb1, J.items0, J.items);
     }
     __syncwarp();
   } else if (warp == kWarpMma) {
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, st = 0, phase = 0;
+      int turn = 0;
       bool ok = true;
-      // 16 values of t: 32 bytes along 128-byte rows, or 16 rows of 128 bytes
-      // (descriptors count in 16 bytes)
-      const uint64_t step_a = P.a_outer ? 128u : 2u, step_b = P.b_outer ? 128u : 2u, step_st = stage_bytes >> 4;
+      const uint64_t step_st = J.stage_bytes >> 4;  // descriptors count in 16 bytes
       const uint64_t da0 = tc::desc128(base, 8192u), db0 = tc::desc128(base + kABytes, 8192u);
       uint64_t da = da0, db = db0;
       // The next stage's barrier is awaited in the middle of a stage's MMAs: the
       // tensor pipe holds about two MMAs, which cover the wait there but not
       // one between stages (720 against 512 cycles a stage of 256 x 256).
-      for (int item = first; item < items && ok; item += step, ++it) {
-        int tm, tn, part;
-        item_of(P, item, tm, tn, part);
-        const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
-        const uint32_t a = it & 1u, d = tmem + a * (uint32_t)P.nt;
-        if (!tc::bar_wait(tc::smem_u32(&B.accempty[a]), ((it >> 1) & 1u) ^ 1u, abort, P.wait_ns) ||
-            !tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, P.wait_ns))
-          break;
-        tc::fence_after();
-        for (int left = s1 - s0; left > 0; --left) {
-          const uint32_t bar = tc::smem_u32(&B.empty[st]);
-          const bool wrap = st + 1 == nstages;
-          tc::mma<CG>(d, da, db, P.idesc, left != s1 - s0);
-          tc::mma<CG>(d, da + step_a, db + step_b, P.idesc, 1u);
-          st = wrap ? 0u : st + 1;
-          phase ^= wrap ? 1u : 0u;
-          ok = left == 1 || tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, P.wait_ns);
+      auto multiply = [&](const Product &P, int from, int to) {
+        // 16 values of t: 32 bytes along 128-byte rows, or 16 rows of 128 bytes
+        const uint64_t step_a = P.a_outer ? 128u : 2u, step_b = P.b_outer ? 128u : 2u;
+        for (; ok; ++turn) {
+          const int item = item_at(turn, slot, slots);
+          if (item >= to) break;
+          int tm, tn, part;
+          item_of(P, item - from, tm, tn, part);
+          const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
+          const uint32_t a = it & 1u, d = tmem + a * (uint32_t)J.nt;
+          if (!tc::bar_wait(tc::smem_u32(&B.accempty[a]), ((it >> 1) & 1u) ^ 1u, abort, limit) ||
+              !tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, limit)) {
+            ok = false;
+            break;
+          }
           tc::fence_after();
-          tc::mma<CG>(d, da + 2 * step_a, db + 2 * step_b, P.idesc, 1u);
-          tc::mma<CG>(d, da + 3 * step_a, db + 3 * step_b, P.idesc, 1u);
-          tc::commit<CG>(bar);
-          if (!ok) break;
-          da = wrap ? da0 : da + step_st;
-          db = wrap ? db0 : db + step_st;
+          for (int left = s1 - s0; left > 0; --left) {
+            const uint32_t bar = tc::smem_u32(&B.empty[st]);
+            const bool wrap = st + 1 == nstages;
+            tc::mma<CG>(d, da, db, P.idesc, left != s1 - s0);
+            tc::mma<CG>(d, da + step_a, db + step_b, P.idesc, 1u);
+            st = wrap ? 0u : st + 1;
+            phase ^= wrap ? 1u : 0u;
+            ok = left == 1 || tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, limit);
+            tc::fence_after();
+            tc::mma<CG>(d, da + 2 * step_a, db + 2 * step_b, P.idesc, 1u);
+            tc::mma<CG>(d, da + 3 * step_a, db + 3 * step_b, P.idesc, 1u);
+            tc::commit<CG>(bar);
+            if (!ok) break;
+            da = wrap ? da0 : da + step_st;
+            db = wrap ? db0 : db + step_st;
+          }
+          if (ok) tc::commit<CG>(tc::smem_u32(&B.accfull[a]));
+          ++it;
         }
-        if (ok) tc::commit<CG>(tc::smem_u32(&B.accfull[a]));
-      }
+      };
+      multiply(J.p[0], 0, J.items0);
+      multiply(J.p[1], J.items0, J.items);
       // every MMA is complete before tensor memory is freed or the pair ends
       tc::commit<CG>(tc::smem_u32(&B.drain));
       const uint64_t t0 = tc::now_ns();
@@ -357,27 +403,35 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     const int lg = warp & 3;  // the quarter of the lanes this warp may read
     const uint32_t lane_base = (uint32_t)(lg * 32) << 16;
     float *stage = reinterpret_cast<float *>(smem + o_staging + (uint32_t)ew * kStaging);
-    const int seg = lane & 3, r8 = lane >> 2, n = (int)E.n;
-    const bool vectors = E.y_vec && E.y_dtype != NR_F32 && (!E.z || E.z_scale || E.z_vec) && (!E.residual || E.residual_vec) &&
-                         !P.partial;
+    const int seg = lane & 3, r8 = lane >> 2;
     const uint32_t accempty0 = tc::map_rank(tc::smem_u32(&B.accempty[0]), 0);
     uint32_t it = 0;
-    for (int item = first; item < items; item += step, ++it) {
+    for (int turn = 0;; ++turn) {
+      const int item = item_at(turn, slot, slots);
+      if (item >= J.items) break;  // later turns are past the end too
+      const bool second = item >= J.items0;
+      const Product &P = J.p[second];
+      const Epilogue E = P.E;  // in registers
+      const int n = (int)E.n;
+      const int64_t rows = P.rows;
+      const bool partial = P.splits > 1;
+      const bool vectors = E.y_vec && E.y_dtype != NR_F32 && (!E.z || E.z_scale || E.z_vec) &&
+                           (!E.residual || E.residual_vec) && !partial;
       int tm, tn, part;
-      item_of(P, item, tm, tn, part);
+      item_of(P, second ? item - J.items0 : item, tm, tn, part);
       const uint32_t a = it & 1u;
       const int64_t i0 = ((int64_t)tm * CG + rank) * kRows + lg * 32;
       // the two warps of a lane quarter take its chunks of 32 columns in turn
-      const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < P.rows ? min(n, (tn + 1) * P.nt) : 0;
-      if (__all_sync(0xffffffffu, tc::bar_wait(tc::smem_u32(&B.accfull[a]), (it >> 1) & 1u, abort, P.wait_ns)) == 0) break;
+      const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < rows ? min(n, (tn + 1) * P.nt) : 0;
+      if (__all_sync(0xffffffffu, tc::bar_wait(tc::smem_u32(&B.accfull[a]), (it >> 1) & 1u, abort, limit)) == 0) break;
       tc::fence_after();
-      const uint32_t acc = tmem + lane_base + a * (uint32_t)P.nt - (uint32_t)(tn * P.nt);
+      const uint32_t acc = tmem + lane_base + a * (uint32_t)J.nt - (uint32_t)(tn * P.nt);
       for (int c = c0; c < c1; c += 64) {
         uint32_t v[32];
         __syncwarp();  // the block's previous readers are done
         tc::ld32(acc + (uint32_t)c, v);
         const int j = c + seg * 8;
-        const bool whole = vectors && c + 32 <= n && i0 + 32 <= P.rows;
+        const bool whole = vectors && c + 32 <= n && i0 + 32 <= rows;
         // meanwhile, what the read-back needs
         float2 b[4];
         uint4 res[4];
@@ -403,10 +457,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             float2 s[4];
             stage_read(stage, lane, u, s);
             const int64_t i = i0 + u * 8 + r8;
-            if (!P.partial) {
-              finish8(E, i, j, i < P.rows, s, b);
-            } else if (i < P.rows && j < n) {  // the pitch is a multiple of 8
-              float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(E.y) + ((int64_t)part * P.rows + i) * E.y_ld + j);
+            if (!partial) {
+              finish8(E, i, j, i < rows, s, b);
+            } else if (i < rows && j < n) {  // the pitch is a multiple of 8
+              float4 *p = reinterpret_cast<float4 *>(P.parts + ((int64_t)part * rows + i) * P.parts_ld + j);
               p[0] = make_float4(s[0].x, s[0].y, s[1].x, s[1].y);
               p[1] = make_float4(s[2].x, s[2].y, s[3].x, s[3].y);
             }
@@ -416,12 +470,13 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       tc::fence_before();
       __syncwarp();
       if (lane == 0) tc::bar_arrive_cluster(accempty0 + a * 8u);
+      ++it;
     }
   }
   tc::fence_before();
   __syncthreads();
   if (tid == 0 && B.abort) {
-    atomicCAS(flag, 0, NR_DEV_TIMEOUT);
+    atomicCAS(J.flag, 0, NR_DEV_TIMEOUT);
     // no MMA waits for the copies in flight any more: a millisecond lets them land
     const uint64_t t0 = tc::now_ns();
     while (tc::now_ns() - t0 < 1000000u) {
@@ -435,26 +490,60 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-// adds the parts' sums in order and finishes them: a thread eight columns, the
-// columns padded to whole groups of 32
-__global__ void __launch_bounds__(256)
-    finish_kernel(const float *parts, int splits, int64_t part_ld, int64_t rows, const Epilogue E) {
-  const int64_t segs = (E.n + kOpsGroup - 1) / kOpsGroup * 4;
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t i = e / segs, j = (e - i * segs) * 8;
-  const bool row_ok = i < rows;
-  float2 v[4] = {}, b[4];
-  if (row_ok && j < E.n) {
+// What is left after the products, in one launch: block ranges add the parts'
+// sums of a split product in order and finish them (a thread eight columns,
+// padded to whole groups of 32), and the rows of column sums that dz_kernel
+// left into dbias (32 columns a block, eight rows at a time).
+struct Finish {
+  Product p[2];
+  int blocks[2];  // of each product; 0: not split
+  const float *sums;
+  int sums_rows;
+  int64_t sums_n;
+  void *dbias;
+  int dbias_dtype;
+};
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Finish F) {
+  __shared__ float sums[8][33];
+  grid_wait();
+  int block = (int)blockIdx.x;
+  const int which = block < F.blocks[0] ? 0 : 1;
+  if (which) block -= F.blocks[0];
+  if (which == 0 || block < F.blocks[1]) {
+    const Product &P = F.p[which];
+    const Epilogue &E = P.E;
+    const int segs = ((int)E.n + kOpsGroup - 1) / kOpsGroup * 4;
+    const int64_t e = (int64_t)block * 256 + threadIdx.x;
+    const int64_t i = e / segs;
+    const int j = (int)(e - i * segs) * 8;
+    const bool row_ok = i < P.rows;
+    float2 v[4] = {}, b[4];
+    if (row_ok && j < (int)E.n) {
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-      const float4 *p = reinterpret_cast<const float4 *>(parts + ((int64_t)s * rows + i) * part_ld + j);
-      const float4 lo = __ldg(p), hi = __ldg(p + 1);
-      v[0] = add2(v[0], make_float2(lo.x, lo.y)), v[1] = add2(v[1], make_float2(lo.z, lo.w));
-      v[2] = add2(v[2], make_float2(hi.x, hi.y)), v[3] = add2(v[3], make_float2(hi.z, hi.w));
+      for (int s = 0; s < P.splits; ++s) {
+        const float4 *p = reinterpret_cast<const float4 *>(P.parts + ((int64_t)s * P.rows + i) * P.parts_ld + j);
+        const float4 lo = p[0], hi = p[1];
+        v[0] = add2(v[0], make_float2(lo.x, lo.y)), v[1] = add2(v[1], make_float2(lo.z, lo.w));
+        v[2] = add2(v[2], make_float2(hi.x, hi.y)), v[3] = add2(v[3], make_float2(hi.z, hi.w));
+      }
     }
+    bias8(E, j, b);
+    finish8(E, i, j, row_ok, v, b);
+    return;
   }
-  bias8(E, (int)j, b);
-  finish8(E, i, (int)j, row_ok, v, b);
+  block -= F.blocks[1];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t j = (int64_t)block * 32 + c;
+  float s = 0.0f;
+  if (j < F.sums_n) {
+#pragma unroll 8
+    for (int p = r; p < F.sums_rows; p += 8) s += F.sums[(int64_t)p * F.sums_n + j];
+  }
+  sums[r][c] = s;
+  __syncthreads();
+  if (r != 0 || j >= F.sums_n) return;
+  for (int q = 1; q < 8; ++q) s += sums[q][c];
+  store_any(F.dbias, j, F.dbias_dtype, s);
 }
 
 // ------------------------------------------------------------ few rows, on CUDA cores
@@ -535,105 +624,112 @@ __global__ void __launch_bounds__(kRowsThreads)
   store_any(E.y, r * E.y_ld + j, E.y_dtype, y);
 }
 
-// ------------------------------------------------------------ dz and dbias
+// ------------------------------------------------------------ dz and the column sums
 // z: values of a type, or a checkpoint's codes and scales
 struct Saved {
   const void *p;
   const uint8_t *scale;
   int64_t ld;
-  int64_t groups;
-  int vec;
+  int groups;
 };
-__device__ __forceinline__ void saved8(const Saved &s, int64_t i, int64_t j, int dtype, int count, float (&v)[8]) {
-  if (!s.scale) {
-    load8(s.p, i * s.ld + j, dtype, s.vec, count, v);
-    return;
-  }
-  const uint2 c = *reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(s.p) + i * s.groups * kOpsGroup + j);
-  const float down = held8_down(s.scale[i * s.groups + (j >> 5)]);
-  float2 p[4];
-  held8_numbers(c.x, p[0], p[1]);
-  held8_numbers(c.y, p[2], p[3]);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    v[2 * q] = p[q].x * down;
-    v[2 * q + 1] = p[q].y * down;
-  }
-}
 
-// dz = dy act'(z) rounded to dtype (unless dz is null), and the column sums of
-// the unrounded values over this block's rows -> parts[blockIdx.y] (unless
-// null). A block takes 256 columns, eight a lane, and its eight warps its rows
-// in turn.
-__global__ void __launch_bounds__(256)
-    dz_kernel(const void *dy, int dy_dtype, int64_t dy_ld, int dy_vec, const Saved z, int act, int64_t m, int64_t n,
-              int rows_per_block, int dtype, uint16_t *dz, int64_t dz_ld, float *parts) {
-  __shared__ float sums[8][32 * 9];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t j = (int64_t)blockIdx.x * 256 + lane * 8;
-  const int count = (int)min((int64_t)8, n - j);
-  const int64_t i0 = (int64_t)blockIdx.y * rows_per_block, i1 = min(m, i0 + rows_per_block);
-  float acc[8] = {};
-  if (count > 0) {
-#pragma unroll 2
-    for (int64_t i = i0 + warp; i < i1; i += 8) {
-      float v[8];
-      load8(dy, i * dy_ld + j, dy_dtype, dy_vec, count, v);
-      if (act != NR_ACT_NONE) {
-        float s[8];
-        saved8(z, i, j, dtype, count, s);
+// dz = dy act'(z) rounded to T (unless dz is null), and the column sums of the
+// unrounded values over a block's rows -> sums[blockIdx.y] (unless null). Bound
+// by memory: dy and z read, dz written. A block's threads: x over columns, eight
+// each, y over rows; a thread takes four rows at a time, all loads first.
+// VEC: n is a multiple of 8 and dy and z take 16-byte accesses.
+constexpr int kDzRows = 4;
+template <bool VEC, typename D, typename T>
+__global__ void __launch_bounds__(256, 2)
+    dz_kernel(const D *dy, int64_t dy_ld, const Saved z, int act, int64_t m, int n, int rows_per_block, T *dz,
+              int64_t dz_ld, float *sums) {
+  __shared__ float part[256 * 8];
+  const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8, count = max(0, min(8, n - j));
+  const int64_t i1 = min(m, ((int64_t)blockIdx.y + 1) * rows_per_block);
+  float2 acc[4] = {};
+  const int step = blockDim.y;
+  grid_launch();
+  for (int64_t i0 = (int64_t)blockIdx.y * rows_per_block + threadIdx.y; i0 < i1 && count > 0; i0 += kDzRows * step) {
+    float v[kDzRows][8], s[kDzRows][8];
+    uint2 c[kDzRows];
+    uint32_t sc[kDzRows];
 #pragma unroll
-        for (int q = 0; q < 8; q += 2) {
-          const float2 d = mul2(make_float2(v[q], v[q + 1]), act_slope2(make_float2(s[q], s[q + 1]), act));
-          v[q] = d.x;
-          v[q + 1] = d.y;
+    for (int u = 0; u < kDzRows; ++u) {
+      const int64_t i = min(i0 + u * step, i1 - 1);
+      load8(dy + i * dy_ld, j, TypeCode<D>::code, VEC, VEC ? 8 : count, v[u]);
+      if (act != NR_ACT_NONE) {
+        if (!z.scale) {
+          load8(static_cast<const T *>(z.p) + i * z.ld, j, TypeCode<T>::code, VEC, VEC ? 8 : count, s[u]);
+        } else {
+          c[u] = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(z.p) + i * z.groups * kOpsGroup + j));
+          sc[u] = __ldg(z.scale + i * z.groups + (j >> 5));
         }
       }
-      if (dz) store8(dz, i * dz_ld + j, dtype, 1, 8, v);  // the pitch is a multiple of 8
+    }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) acc[q] += v[q];
+    for (int u = 0; u < kDzRows; ++u) {
+      const int64_t i = i0 + u * step;
+      if (i >= i1) break;
+      float2 d[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) d[q] = make_float2(v[u][2 * q], v[u][2 * q + 1]);
+      if (act != NR_ACT_NONE) {
+        float2 p[4];
+        if (z.scale) {
+          held8_numbers(c[u].x, p[0], p[1]);
+          held8_numbers(c[u].y, p[2], p[3]);
+          const float down = held8_down(sc[u]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) p[q] = mul2(p[q], both(down));
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) p[q] = make_float2(s[u][2 * q], s[u][2 * q + 1]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) d[q] = mul2(d[q], act_slope2(p[q], act));
+      }
+      // the pitch is a multiple of 8
+      if (dz) *reinterpret_cast<uint4 *>(dz + i * dz_ld + j) = pack8(d, TypeCode<T>::code);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[q] = add2(acc[q], d[q]);
     }
   }
-  if (!parts) return;
+  if (!sums) return;
+  const int bx = blockDim.x * 8;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) sums[warp][lane * 9 + q] = acc[q];
+  for (int q = 0; q < 4; ++q)
+    *reinterpret_cast<float2 *>(part + threadIdx.y * bx + threadIdx.x * 8 + 2 * q) = acc[q];
   __syncthreads();
-  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (col >= n) return;
+  const int t = threadIdx.y * blockDim.x + threadIdx.x, col = blockIdx.x * bx + t;
+  if (t >= bx || col >= n) return;
   float s = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 8; ++w) s += sums[w][(threadIdx.x >> 3) * 9 + (threadIdx.x & 7)];
-  parts[(int64_t)blockIdx.y * n + col] = s;
+  for (int r = 0; r < (int)blockDim.y; ++r) s += part[r * bx + t];
+  sums[(int64_t)blockIdx.y * n + col] = s;
 }
 
-// dbias[j] = the sum of parts[.][j]: 32 columns a block, eight rows of parts at a time
-__global__ void __launch_bounds__(256) dbias_kernel(const float *parts, int count, int64_t n, void *dbias, int dtype) {
-  __shared__ float sums[8][33];
-  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t j = (int64_t)blockIdx.x * 32 + c;
-  float s = 0.0f;
-  if (j < n) {
-#pragma unroll 4
-    for (int p = r; p < count; p += 8) s += parts[(int64_t)p * n + j];
-  }
-  sums[r][c] = s;
-  __syncthreads();
-  if (r != 0 || j >= n) return;
-  for (int q = 1; q < 8; ++q) s += sums[q][c];
-  store_any(dbias, j, dtype, s);
-}
-
-// rows of 16-bit values at any pitch and alignment -> pitch d_ld (a multiple of 8)
-__global__ void __launch_bounds__(256)
-    pack_kernel(const uint16_t *__restrict__ s, int64_t s_ld, int64_t rows, int64_t cols, uint16_t *d, int64_t d_ld) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t segs = d_ld / 8, i = e / segs, j = (e - i * segs) * 8;
-  if (i >= rows) return;
+// rows of 16-bit values at any pitch and alignment -> pitch d_ld (a multiple of
+// 8), for up to two matrices a launch
+struct Pack {
+  const uint16_t *s[2];
+  uint16_t *d[2];
+  int64_t s_ld[2], rows[2];
+  int cols[2], d_ld[2];
+  int64_t blocks0;
+};
+__global__ void __launch_bounds__(256) pack_kernel(const Pack K) {
+  grid_launch();
+  const int which = (int64_t)blockIdx.x >= K.blocks0;
+  const int64_t e = ((int64_t)blockIdx.x - (which ? K.blocks0 : 0)) * 256 + threadIdx.x;
+  const int segs = K.d_ld[which] / 8, cols = K.cols[which];
+  const int64_t i = e / segs;
+  const int j = (int)(e - i * segs) * 8;
+  if (i >= K.rows[which]) return;
+  const uint16_t *s = K.s[which] + i * K.s_ld[which] + j;
   uint32_t v[4] = {};
 #pragma unroll
   for (int q = 0; q < 8; ++q)
-    if (j + q < cols) v[q >> 1] |= (uint32_t)s[i * s_ld + j + q] << (16 * (q & 1));
-  *reinterpret_cast<uint4 *>(d + i * d_ld + j) = make_uint4(v[0], v[1], v[2], v[3]);
+    if (j + q < cols) v[q >> 1] |= (uint32_t)__ldg(s + q) << (16 * (q & 1));
+  *reinterpret_cast<uint4 *>(K.d[which] + i * K.d_ld[which] + j) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // ------------------------------------------------------------ host
@@ -680,39 +776,40 @@ struct Cut {
   int cg, nt, splits;
 };
 
-uint32_t stage_bytes(const Cut &c) { return kABytes + (uint32_t)(c.nt / c.cg) * kSlice * 2; }
 constexpr uint32_t kSmemMax = 232448;
-int stage_count(const Cut &c) {
-  const uint32_t fixed = 1024u + kEpiWarps * kStaging + (uint32_t)sizeof(Bars);
-  const int s = (int)((kSmemMax - fixed) / stage_bytes(c));
-  return s < kStagesMax ? s : kStagesMax;
-}
+uint32_t cut_bytes(const Cut &c) { return kABytes + (uint32_t)(c.nt / c.cg) * kSlice * 2; }
 
 // The cut with the least estimated time, in cycles of an SM: a slice of a tile
-// costs its MMAs (128 x nt x 64 products at 8192 flop a cycle) or the copy of
-// its operands (48 bytes a cycle an SM), whichever is longer; an item 1500
-// cycles more; parts of t their sums' way through L2 (2 KB a cycle over the GPU).
-Cut choose(int64_t rows, int64_t n, int64_t slices, bool b_outer, int sms) {
+// costs its MMAs (128 x nt x 64 products at 8192 flop a cycle, of which 0.85
+// was reached) or the copy of its operands (56 bytes a cycle an SM), whichever is
+// longer; an item 1500 cycles more; parts of t their sums' way through L2 (2 KB a
+// cycle over the GPU) and the launch that adds them. cg 0: either.
+Cut choose(int64_t rows, int64_t n, int64_t slices, bool b_outer, int cg_only, int sms, float *cost = nullptr) {
+  static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
   Cut best = {1, 64, 1};
-  double least = 1e30;
-  for (int cg = 1; cg <= 2; ++cg)
+  float least = 1e30f;
+  for (int cg = 1; cg <= 2; ++cg) {
+    if (cg_only ? cg != cg_only : cg == 2 && rows <= kRows) continue;
+    const int64_t tm = ceil_div(rows, (int64_t)kRows * cg), slot = sms / cg;
     for (int nt = 32; nt <= 256; nt *= 2) {
-      if (cg == 2 && (nt < 128 || rows <= kRows)) continue;
+      if (cg == 2 && nt < 128) continue;
       if (b_outer && nt / cg < 64) continue;
-      if (nt > 32 && nt / 2 >= n && !(b_outer && nt / cg == 64)) continue;  // half of it would do
-      const Cut c0 = {cg, nt, 1};
-      const double tiles = (double)ceil_div(rows, (int64_t)kRows * cg) * (double)ceil_div(n, nt);
-      const double feed = stage_bytes(c0) / 48.0, mma = 2.0 * nt, slot = sms / cg;
-      for (int sp = 1; sp <= 32 && (sp == 1 || slices / sp >= 4); ++sp) {
-        const double items = tiles * sp, waves = (double)ceil_div((int64_t)items, (int64_t)slot);
-        double t = waves * ((double)ceil_div(slices, sp) * (feed > mma ? feed : mma) + 1500.0);
-        if (sp > 1) t += 4000.0 + 8.0 * (double)rows * (double)n * sp / 2048.0;
+      if (nt > 32 && nt / 2 >= n && !(b_outer && nt / cg == 64) && !(cg == 2 && nt == 128)) continue;  // half of it would do
+      const int64_t tiles = tm * ceil_div(n, nt);
+      const float feed = (float)cut_bytes({cg, nt, 1}) / 56.0f, mma = 2.35f * (float)nt, each = feed > mma ? feed : mma;
+      for (int sp : kSplits) {
+        if (sp > 1 && (slices / sp < 4 || tiles * (sp - 1) > 4 * slot)) break;
+        const float waves = (float)ceil_div(tiles * sp, slot);
+        float t = waves * ((float)ceil_div(slices, sp) * each + 1500.0f);
+        if (sp > 1) t += 4000.0f + 8.0f * (float)rows * (float)n * (float)sp / 2048.0f;
         if (t < least) {
           least = t;
           best = {cg, nt, sp};
         }
       }
     }
+  }
+  if (cost) *cost = least;
   return best;
 }
 
@@ -722,9 +819,35 @@ int64_t parts_bytes(const Cut &c, int64_t rows, int64_t n) {
 
 int64_t wait_limit = kWaitNs;  // nr_ops_wait_limit
 
+// a launch that may begin before the previous one of the call has ended: its
+// kernel waits (grid_wait) before it touches memory
+template <typename... K, typename... A>
+cudaError_t launch(void (*kernel)(K...), unsigned grid, dim3 block, uint32_t smem, cudaStream_t s, bool follows, A &&...a) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = block;
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at;
+  c.numAttrs = follows ? 1 : 0;
+  return cudaLaunchKernelEx(&c, kernel, static_cast<K>(a)...);
+}
+
+// an operand pair, its cut and what becomes of C
+struct Task {
+  Operand A, B;
+  int64_t rows, inner;
+  Cut c;
+  Epilogue E;
+  float *parts;  // scratch of parts_bytes(c, rows, E.n)
+};
+
 template <int CG>
-cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &mb, const Product &P, const Epilogue &E, uint32_t smem,
-                           int grid, int device, int *flag, cudaStream_t s) {
+cudaError_t launch_product(const CUtensorMap (&m)[4], const Job &J, uint32_t smem, int grid, int device, bool follows,
+                           cudaStream_t s) {
   static bool ready[64];  // the attribute is set once a device
   if (!ready[device]) {
     const cudaError_t e =
@@ -732,57 +855,83 @@ cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &mb, const P
     if (e != cudaSuccess) return e;
     ready[device] = true;
   }
-  product_kernel<CG><<<grid, kThreads, smem, s>>>(ma, mb, P, E, flag);
-  return cudaGetLastError();
+  return launch(product_kernel<CG>, (unsigned)grid, dim3(kThreads), smem, s, follows, m[0], m[1], m[2], m[3], J);
 }
 
-// C [rows x E.n] = A B^T over t < inner, through E; parts: scratch of parts_bytes(c, rows, E.n)
-nr_status product(const Operand &A, const Operand &B, int64_t rows, int64_t inner, const Cut &c, const Epilogue &E,
-                  void *parts, int device, cudaStream_t s) {
-  int *flag = nullptr;
-  cudaError_t e = nr_ops_flag(device, &flag);
-  if (e != cudaSuccess) return cuda_status(e);
-  CUtensorMap ma, mb;
-  if (!make_map(&ma, A, E.dtype, A.outer ? kSlice : kRows) ||
-      !make_map(&mb, B, E.dtype, B.outer ? kSlice : c.nt / c.cg))
-    return NR_ERR_CUDA;
-  Product P = {};
-  P.rows = rows;
-  P.tiles_m = (int)ceil_div(rows, (int64_t)kRows * c.cg);
-  P.tiles_n = (int)ceil_div(E.n, c.nt);
-  P.nt = c.nt;
-  P.stages = stage_count(c);
-  P.slices = (int)ceil_div(inner, kSlice);
-  P.splits = c.splits;
-  P.a_outer = A.outer;
-  P.b_outer = B.outer;
-  P.idesc = tc::idesc_f16(kRows * c.cg, c.nt, E.dtype == NR_BF16, A.outer, B.outer);
-  P.partial = c.splits > 1;
-  P.wait_ns = wait_limit;
-  Epilogue X = E;
-  if (P.partial) {
-    X.y = parts;
-    X.y_ld = round_up(E.n, 8);
+// The products of one or two tasks (of the same CTAs a tile) in one launch, and
+// what is left to finish, with the column sums' last addition, in another.
+// follows: the call has launched before.
+nr_status products(const Task *t, int count, Finish &F, int device, bool follows, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  Job J = {};
+  if (count > 0) {
+    e = nr_ops_flag(device, &J.flag);
+    if (e != cudaSuccess) return cuda_status(e);
+    CUtensorMap maps[4];
+    const int cg = t[0].c.cg;
+    for (int q = 0; q < count; ++q) {
+      const Task &k = t[q];
+      if (!make_map(&maps[2 * q], k.A, k.E.dtype, k.A.outer ? kSlice : kRows) ||
+          !make_map(&maps[2 * q + 1], k.B, k.E.dtype, k.B.outer ? kSlice : k.c.nt / cg))
+        return NR_ERR_CUDA;
+      Product &P = J.p[q];
+      P.rows = k.rows;
+      P.tiles_m = (int)ceil_div(k.rows, (int64_t)kRows * cg);
+      P.tiles_n = (int)ceil_div(k.E.n, k.c.nt);
+      P.nt = k.c.nt;
+      P.slices = (int)ceil_div(k.inner, kSlice);
+      P.splits = k.c.splits;
+      P.a_outer = k.A.outer;
+      P.b_outer = k.B.outer;
+      P.idesc = tc::idesc_f16(kRows * cg, k.c.nt, k.E.dtype == NR_BF16, k.A.outer, k.B.outer);
+      P.parts = k.parts;
+      P.parts_ld = round_up(k.E.n, 8);
+      P.E = k.E;
+      const int64_t items = (int64_t)P.tiles_m * P.tiles_n * P.splits;
+      if (items > (int64_t)1 << 29) return NR_ERR_INVALID_ARG;
+      J.items += (int)items;
+      if (q == 0) J.items0 = (int)items;
+      if (k.c.nt > J.nt) J.nt = k.c.nt;
+      if (cut_bytes(k.c) > J.stage_bytes) J.stage_bytes = cut_bytes(k.c);
+      if (P.splits > 1) {
+        F.p[q] = P;
+        F.blocks[q] = (int)ceil_div(k.rows * ceil_div(k.E.n, kOpsGroup) * 4, 256);
+      }
+    }
+    if (count == 1) maps[2] = maps[0], maps[3] = maps[1];
+    const uint32_t fixed = 1024u + kEpiWarps * kStaging + (uint32_t)sizeof(Bars);
+    J.stages = (int)((kSmemMax - fixed) / J.stage_bytes);
+    if (J.stages > kStagesMax) J.stages = kStagesMax;
+    J.wait_ns = wait_limit;
+    const int slots = nr_ops_sms(device) / cg;
+    const int grid = (J.items < slots ? J.items : slots) * cg;
+    const uint32_t smem = fixed + (uint32_t)J.stages * J.stage_bytes;
+    e = cg == 1 ? launch_product<1>(maps, J, smem, grid, device, follows, s)
+                : launch_product<2>(maps, J, smem, grid, device, follows, s);
+    follows = true;
   }
-  const int64_t items = (int64_t)P.tiles_m * P.tiles_n * P.splits, slots = nr_ops_sms(device) / c.cg;
-  if (items > (int64_t)1 << 30) return NR_ERR_INVALID_ARG;
-  const int grid = (int)(items < slots ? items : slots) * c.cg;
-  const uint32_t smem = 1024u + (uint32_t)P.stages * stage_bytes(c) + kEpiWarps * kStaging + (uint32_t)sizeof(Bars);
-  e = c.cg == 1 ? launch_product<1>(ma, mb, P, X, smem, grid, device, flag, s)
-                : launch_product<2>(ma, mb, P, X, smem, grid, device, flag, s);
-  if (e == cudaSuccess && P.partial) {
-    const int64_t threads = rows * ceil_div(E.n, kOpsGroup) * 4;
-    finish_kernel<<<(unsigned)ceil_div(threads, 256), 256, 0, s>>>(static_cast<const float *>(parts), c.splits, X.y_ld,
-                                                                   rows, E);
-    e = cudaGetLastError();
-  }
+  const int64_t blocks = (int64_t)F.blocks[0] + F.blocks[1] + (F.dbias ? ceil_div(F.sums_n, 32) : 0);
+  if (e == cudaSuccess && blocks > 0) e = launch(finish_kernel, (unsigned)blocks, dim3(256), 0, s, follows, F);
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }
 
-cudaError_t pack(const void *src, int64_t ld, int64_t rows, int64_t cols, void *dst, cudaStream_t s) {
-  const int64_t d_ld = round_up(cols, 8);
-  pack_kernel<<<(unsigned)ceil_div(rows * (d_ld / 8), 256), 256, 0, s>>>(static_cast<const uint16_t *>(src), ld, rows,
-                                                                         cols, static_cast<uint16_t *>(dst), d_ld);
+// one or two matrices into aligned rows
+cudaError_t pack(Operand *o, void *const *dst, int count, cudaStream_t s) {
+  Pack K = {};
+  int64_t blocks = 0;
+  for (int q = 0; q < count; ++q) {
+    K.s[q] = static_cast<const uint16_t *>(o[q].p);
+    K.d[q] = static_cast<uint16_t *>(dst[q]);
+    K.s_ld[q] = o[q].ld;
+    K.rows[q] = o[q].rows;
+    K.cols[q] = (int)o[q].cols;
+    K.d_ld[q] = (int)round_up(o[q].cols, 8);
+    blocks += ceil_div(o[q].rows * (K.d_ld[q] / 8), 256);
+    if (q == 0) K.blocks0 = blocks;
+    o[q].p = dst[q];
+    o[q].ld = K.d_ld[q];
+  }
+  pack_kernel<<<(unsigned)blocks, 256, 0, s>>>(K);
   return cudaGetLastError();
 }
 
@@ -836,7 +985,7 @@ ForwardPlan plan_forward(const nr_linear *a, int device) {
   }
   if (!mappable(f.x)) f.x_at = s.take(a->m * round_up(a->k, 8) * 2);
   if (!mappable(f.w)) f.w_at = s.take(a->n * round_up(a->k, 8) * 2);
-  f.cut = choose(a->m, a->n, ceil_div(a->k, kSlice), false, nr_ops_sms(device));
+  f.cut = choose(a->m, a->n, ceil_div(a->k, kSlice), false, 0, nr_ops_sms(device));
   if (f.cut.splits > 1) f.parts_at = s.take(parts_bytes(f.cut, a->m, a->n));
   f.bytes = s.at;
   return f;
@@ -865,18 +1014,29 @@ void launch_rows_any(const nr_linear *a, const Epilogue &E, int sms, cudaStream_
   else launch_rows<8, T>(a, E, sms, s);
 }
 
-// rows a block of dz_kernel takes: enough blocks for the GPU, at most 256 parts to add
-int dz_rows(int64_t m, int64_t n, int sms) {
-  const int64_t want = ceil_div((int64_t)sms * 8, ceil_div(n, 256));
-  const int64_t blocks = want < 256 ? want : 256;
-  const int64_t r = round_up(ceil_div(m, blocks), 8);
-  return (int)(r < 8 ? 8 : r);
+// dz_kernel's blocks: threads across up to 256 columns, rows of few columns share a
+// block; enough blocks for the GPU, at most 256 rows of column sums to add
+struct DzCut {
+  dim3 block;
+  int gx, gy, rows;
+};
+DzCut cut_dz(int64_t m, int64_t n, int sms) {
+  DzCut c;
+  unsigned bx = 4;
+  while (bx < 32 && (int64_t)bx * 8 < n) bx *= 2;
+  c.block = dim3(bx, 256 / bx);
+  c.gx = (int)ceil_div(n, (int64_t)bx * 8);
+  const int64_t most = ceil_div((int64_t)sms * 4, c.gx);
+  const int64_t step = kDzRows * (int64_t)c.block.y;
+  c.rows = (int)round_up(ceil_div(m, most < 256 ? most : 256), step);
+  c.gy = (int)ceil_div(m, c.rows);
+  return c;
 }
 
 struct BackwardPlan {
   bool make_dz;  // else dy serves as it is
   Operand dz, x, w;
-  int rows = 0, blocks = 0;
+  DzCut cut;
   int64_t dz_at = -1, x_at = -1, w_at = -1, sums_at = -1, dx_at = -1, dw_at = -1, bytes = 0;
   Cut dx = {1, 64, 1}, dw = {1, 64, 1};
 };
@@ -894,31 +1054,44 @@ BackwardPlan plan_backward(const nr_linear *a, int device) {
     b.dz_at = s.take(m * round_up(n, 8) * 2);
     b.dz.ld = round_up(n, 8);
   }
-  b.rows = dz_rows(m, n, sms);
-  b.blocks = (int)ceil_div(m, b.rows);
-  if (a->dbias) b.sums_at = s.take((int64_t)b.blocks * n * 4);
+  b.cut = cut_dz(m, n, sms);
+  if (a->dbias) b.sums_at = s.take((int64_t)b.cut.gy * n * 4);
   if (a->dw && (a->x_scale || !mappable(b.x))) {
     b.x_at = s.take(m * round_up(k, 8) * 2);
-    b.x.ld = round_up(k, 8);
+    if (a->x_scale) b.x.ld = round_up(k, 8);
   }
-  if (a->dx && !mappable(b.w)) {
-    b.w_at = s.take(n * round_up(k, 8) * 2);
-    b.w.ld = round_up(k, 8);
+  if (a->dx && !mappable(b.w)) b.w_at = s.take(n * round_up(k, 8) * 2);
+  // both in one launch, so of the same CTAs a tile
+  float cost[2] = {0.0f, 0.0f};
+  const int only = a->dx && a->dw ? 2 : 0;
+  const int64_t sx = ceil_div(n, kSlice), sw = ceil_div(m, kSlice);
+  if (a->dx) b.dx = choose(m, k, sx, true, only, sms, &cost[0]);
+  if (a->dw) b.dw = choose(n, k, sw, true, only, sms, &cost[1]);
+  if (only) {
+    float c1[2];
+    const Cut dx1 = choose(m, k, sx, true, 1, sms, &c1[0]), dw1 = choose(n, k, sw, true, 1, sms, &c1[1]);
+    if (c1[0] + c1[1] < cost[0] + cost[1]) b.dx = dx1, b.dw = dw1;
   }
-  // the two products run one after the other and share the parts' scratch
-  int64_t parts = 0;
-  if (a->dx) {
-    b.dx = choose(m, k, ceil_div(n, kSlice), true, sms);
-    parts = parts_bytes(b.dx, m, k);
-  }
-  if (a->dw) {
-    b.dw = choose(n, k, ceil_div(m, kSlice), true, sms);
-    const int64_t p = parts_bytes(b.dw, n, k);
-    parts = p > parts ? p : parts;
-  }
-  if (parts) b.dx_at = b.dw_at = s.take(parts);
+  if (a->dx && b.dx.splits > 1) b.dx_at = s.take(parts_bytes(b.dx, m, k));
+  if (a->dw && b.dw.splits > 1) b.dw_at = s.take(parts_bytes(b.dw, n, k));
   b.bytes = s.at;
   return b;
+}
+
+template <bool VEC, typename D, typename T>
+void launch_dz(const nr_linear *a, const BackwardPlan &b, const Saved &z, void *dz, float *sums, cudaStream_t s) {
+  dz_kernel<VEC, D, T><<<dim3((unsigned)b.cut.gx, (unsigned)b.cut.gy), b.cut.block, 0, s>>>(
+      static_cast<const D *>(a->dy), a->dy_ld, z, (int)a->act, a->m, (int)a->n, b.cut.rows, static_cast<T *>(dz), b.dz.ld,
+      sums);
+}
+template <typename T>
+void launch_dz_any(const nr_linear *a, const BackwardPlan &b, const Saved &z, void *dz, float *sums, cudaStream_t s) {
+  const bool vec = a->n % 8 == 0 && vec_ok(a->dy, a->dy_ld, a->y_dtype) &&
+                   (a->act == NR_ACT_NONE || z.scale || vec_ok(a->z, a->z_ld, a->dtype));
+  if (a->y_dtype == NR_F32)
+    vec ? launch_dz<true, float, T>(a, b, z, dz, sums, s) : launch_dz<false, float, T>(a, b, z, dz, sums, s);
+  else
+    vec ? launch_dz<true, T, T>(a, b, z, dz, sums, s) : launch_dz<false, T, T>(a, b, z, dz, sums, s);
 }
 
 void *at(void *ws, int64_t o) { return o < 0 ? nullptr : static_cast<char *>(ws) + o; }
@@ -966,19 +1139,20 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
     if (e != cudaSuccess) return cuda_status(e);
     return a->z_scale ? nr_checkpoint8_write(E.z, NR_F32, a->m, a->n, a->n, a->z, a->z_scale, device, stream) : NR_OK;
   }
-  cudaError_t e = cudaSuccess;
-  if (f.x_at >= 0) {
-    e = pack(a->x, a->x_ld, a->m, a->k, at(ws, f.x_at), s);
-    f.x.p = at(ws, f.x_at);
-    f.x.ld = round_up(a->k, 8);
+  Operand o[2];
+  void *dst[2];
+  int packs = 0;
+  if (f.x_at >= 0) o[packs] = f.x, dst[packs++] = at(ws, f.x_at);
+  if (f.w_at >= 0) o[packs] = f.w, dst[packs++] = at(ws, f.w_at);
+  if (packs) {
+    const cudaError_t e = pack(o, dst, packs, s);
+    if (e != cudaSuccess) return cuda_status(e);
+    if (f.x_at >= 0) f.x = o[0];
+    if (f.w_at >= 0) f.w = o[packs - 1];
   }
-  if (e == cudaSuccess && f.w_at >= 0) {
-    e = pack(a->w, a->w_ld, a->n, a->k, at(ws, f.w_at), s);
-    f.w.p = at(ws, f.w_at);
-    f.w.ld = round_up(a->k, 8);
-  }
-  if (e != cudaSuccess) return cuda_status(e);
-  return product(f.x, f.w, a->m, a->k, f.cut, E, at(ws, f.parts_at), device, s);
+  Finish F = {};
+  const Task t = {f.x, f.w, a->m, a->k, f.cut, E, static_cast<float *>(at(ws, f.parts_at))};
+  return products(&t, 1, F, device, packs > 0, s);
 }
 
 extern "C" int64_t nr_linear_backward_workspace(const nr_linear *a, int device) {
@@ -1000,55 +1174,63 @@ extern "C" nr_status nr_linear_backward(const nr_linear *a, int device, void *ws
     if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, (size_t)n * type_bytes(a->bias_dtype), s);
     return e == cudaSuccess ? NR_OK : cuda_status(e);
   }
+  bool follows = false;  // a launch of this call has been made
+  if (a->dw && a->x_scale) {
+    const nr_status st =
+        nr_checkpoint8_read(a->x, a->x_scale, m, k, (int)a->x_act, at(ws, b.x_at), dt, b.x.ld, device, stream);
+    if (st != NR_OK) return st;
+    b.x.p = at(ws, b.x_at);
+  }
+  Operand o[2];
+  void *dst[2];
+  int packs = 0;
+  const bool pack_x = a->dw && !a->x_scale && b.x_at >= 0, pack_w = a->dx && b.w_at >= 0;
+  if (pack_x) o[packs] = b.x, dst[packs++] = at(ws, b.x_at);
+  if (pack_w) o[packs] = b.w, dst[packs++] = at(ws, b.w_at);
+  if (packs) {
+    e = pack(o, dst, packs, s);
+    if (e != cudaSuccess) return cuda_status(e);
+    if (pack_x) b.x = o[0];
+    if (pack_w) b.w = o[packs - 1];
+  }
+  Finish F = {};
   if (b.dz_at >= 0 || a->dbias) {
-    const int vec = a->y_dtype == NR_F32 ? vec_ok(a->dy, a->dy_ld, NR_F32) : vec_ok(a->dy, a->dy_ld, dt);
-    const Saved z = {a->z, static_cast<const uint8_t *>(a->z_scale), a->z_ld, ceil_div(n, kOpsGroup),
-                     vec_ok(a->z, a->z_ld, dt)};
+    const Saved z = {a->z, static_cast<const uint8_t *>(a->z_scale), a->z_ld, (int)ceil_div(n, kOpsGroup)};
     float *sums = static_cast<float *>(at(ws, b.sums_at));
-    dz_kernel<<<dim3((unsigned)ceil_div(n, 256), (unsigned)b.blocks), 256, 0, s>>>(
-        a->dy, (int)a->y_dtype, a->dy_ld, vec, z, (int)a->act, m, n, b.rows, dt,
-        static_cast<uint16_t *>(at(ws, b.dz_at)), b.dz.ld, sums);
-    if (a->dbias)
-      dbias_kernel<<<(unsigned)ceil_div(n, 32), 256, 0, s>>>(sums, b.blocks, n, a->dbias, (int)a->bias_dtype);
+    if (dt == NR_F16) launch_dz_any<__half>(a, b, z, at(ws, b.dz_at), sums, s);
+    else launch_dz_any<__nv_bfloat16>(a, b, z, at(ws, b.dz_at), sums, s);
     e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_status(e);
     if (b.dz_at >= 0) b.dz.p = at(ws, b.dz_at);
+    follows = true;
+    if (a->dbias) {
+      F.sums = sums;
+      F.sums_rows = b.cut.gy;
+      F.sums_n = n;
+      F.dbias = a->dbias;
+      F.dbias_dtype = (int)a->bias_dtype;
+    }
   }
+  Task t[2];
+  int count = 0;
   Epilogue E = {};
   E.dtype = E.y_dtype = dt;
   E.n = k;
   if (a->dx) {
-    if (b.w_at >= 0) {
-      e = pack(a->w, a->w_ld, n, k, at(ws, b.w_at), s);
-      if (e != cudaSuccess) return cuda_status(e);
-      b.w.p = at(ws, b.w_at);
-    }
     E.y = a->dx;
     E.y_ld = a->dx_ld;
     E.y_vec = vec_ok(E.y, E.y_ld, dt);
-    const nr_status st = product(b.dz, b.w, m, n, b.dx, E, at(ws, b.dx_at), device, s);
-    if (st != NR_OK) return st;
+    t[count++] = {b.dz, b.w, m, n, b.dx, E, static_cast<float *>(at(ws, b.dx_at))};
   }
   if (a->dw) {
-    if (b.x_at >= 0) {
-      if (a->x_scale) {
-        const nr_status st =
-            nr_checkpoint8_read(a->x, a->x_scale, m, k, (int)a->x_act, at(ws, b.x_at), dt, b.x.ld, device, stream);
-        if (st != NR_OK) return st;
-      } else {
-        e = pack(a->x, a->x_ld, m, k, at(ws, b.x_at), s);
-        if (e != cudaSuccess) return cuda_status(e);
-      }
-      b.x.p = at(ws, b.x_at);
-    }
     E.y = a->dw;
     E.y_ld = k;
     E.y_vec = vec_ok(E.y, E.y_ld, dt);
     Operand dzt = b.dz;
     dzt.outer = true;
-    return product(dzt, b.x, n, m, b.dw, E, at(ws, b.dw_at), device, s);
+    t[count++] = {dzt, b.x, n, m, b.dw, E, static_cast<float *>(at(ws, b.dw_at))};
   }
-  return NR_OK;
+  return products(t, count, F, device, follows, s);
 }
 
 extern "C" nr_status nr_ops_wait_limit(int64_t us) {
