@@ -10,32 +10,6 @@ namespace {
 
 constexpr int kThreads = 256, kBlocks = 6, kBatch = 4;  // blocks an SM, rows at a time
 
-// eight values of a row as they lie in memory (vec: 16-byte accesses)
-template <typename T>
-struct Eight {
-  uint32_t r[sizeof(T) == 4 ? 8 : 4];
-};
-template <typename T>
-__device__ __forceinline__ Eight<T> read_eight(const T *p, bool vec, int count) {
-  Eight<T> o = {};
-  if (vec && count == 8) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
-    o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
-    if (sizeof(T) == 4) {
-      const uint4 b = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
-      o.r[4 % (sizeof(T) * 2)] = b.x, o.r[5 % (sizeof(T) * 2)] = b.y;
-      o.r[6 % (sizeof(T) * 2)] = b.z, o.r[7 % (sizeof(T) * 2)] = b.w;
-    }
-    return o;
-  }
-#pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (q < count) {
-      if (sizeof(T) == 4) o.r[q % (sizeof(T) * 2)] = __ldg(reinterpret_cast<const uint32_t *>(p) + q);
-      else o.r[q >> 1] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + q) << (16 * (q & 1));
-    }
-  return o;
-}
 // the fp32 bits of the largest magnitude: 16-bit types are ordered like their
 // bits without the sign
 template <typename T>
@@ -52,13 +26,6 @@ __device__ __forceinline__ uint32_t largest(const Eight<T> &o) {
   top = max(top & 0xffffu, top >> 16);
   return __float_as_uint(unpack2(top, TypeCode<T>::code).x);
 }
-template <typename T>
-__device__ __forceinline__ float2 pair_of(const Eight<T> &o, int p) {
-  if (sizeof(T) == 4)
-    return make_float2(__uint_as_float(o.r[2 * p % (sizeof(T) * 2)]), __uint_as_float(o.r[(2 * p + 1) % (sizeof(T) * 2)]));
-  return unpack2(o.r[p], TypeCode<T>::code);
-}
-
 // Threads of a block: x along a row (eight columns each, four threads a group),
 // y over rows; a thread takes kBatch rows at a time, all their loads first.
 template <typename T>

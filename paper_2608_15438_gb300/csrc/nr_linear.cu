@@ -640,7 +640,7 @@ struct Saved {
 // VEC: n is a multiple of 8 and dy and z take 16-byte accesses.
 constexpr int kDzRows = 4;
 template <bool VEC, typename D, typename T>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, 3)
     dz_kernel(const D *dy, int64_t dy_ld, const Saved z, int act, int64_t m, int n, int rows_per_block, T *dz,
               int64_t dz_ld, float *sums) {
   __shared__ float part[256 * 8];
@@ -650,19 +650,24 @@ __global__ void __launch_bounds__(256, 2)
   const int step = blockDim.y;
   grid_launch();
   for (int64_t i0 = (int64_t)blockIdx.y * rows_per_block + threadIdx.y; i0 < i1 && count > 0; i0 += kDzRows * step) {
-    float v[kDzRows][8], s[kDzRows][8];
-    uint2 c[kDzRows];
-    uint32_t sc[kDzRows];
+    Eight<D> v[kDzRows];
+    Eight<T> s[kDzRows];
+    float down[kDzRows];
+    const int there = VEC ? 8 : count;
 #pragma unroll
-    for (int u = 0; u < kDzRows; ++u) {
-      const int64_t i = min(i0 + u * step, i1 - 1);
-      load8(dy + i * dy_ld, j, TypeCode<D>::code, VEC, VEC ? 8 : count, v[u]);
-      if (act != NR_ACT_NONE) {
-        if (!z.scale) {
-          load8(static_cast<const T *>(z.p) + i * z.ld, j, TypeCode<T>::code, VEC, VEC ? 8 : count, s[u]);
-        } else {
-          c[u] = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(z.p) + i * z.groups * kOpsGroup + j));
-          sc[u] = __ldg(z.scale + i * z.groups + (j >> 5));
+    for (int u = 0; u < kDzRows; ++u) v[u] = read_eight<D>(dy + min(i0 + u * step, i1 - 1) * dy_ld + j, VEC, there);
+    if (act != NR_ACT_NONE) {
+      if (!z.scale) {
+#pragma unroll
+        for (int u = 0; u < kDzRows; ++u)
+          s[u] = read_eight<T>(static_cast<const T *>(z.p) + min(i0 + u * step, i1 - 1) * z.ld + j, VEC, there);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kDzRows; ++u) {
+          const int64_t i = min(i0 + u * step, i1 - 1);
+          const uint2 c = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(z.p) + i * z.groups * kOpsGroup + j));
+          s[u].r[0] = c.x, s[u].r[1] = c.y;
+          down[u] = held8_down(__ldg(z.scale + i * z.groups + (j >> 5)));
         }
       }
     }
@@ -672,18 +677,17 @@ __global__ void __launch_bounds__(256, 2)
       if (i >= i1) break;
       float2 d[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) d[q] = make_float2(v[u][2 * q], v[u][2 * q + 1]);
+      for (int q = 0; q < 4; ++q) d[q] = pair_of<D>(v[u], q);
       if (act != NR_ACT_NONE) {
         float2 p[4];
         if (z.scale) {
-          held8_numbers(c[u].x, p[0], p[1]);
-          held8_numbers(c[u].y, p[2], p[3]);
-          const float down = held8_down(sc[u]);
+          held8_numbers(s[u].r[0], p[0], p[1]);
+          held8_numbers(s[u].r[1], p[2], p[3]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) p[q] = mul2(p[q], both(down));
+          for (int q = 0; q < 4; ++q) p[q] = mul2(p[q], both(down[u]));
         } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) p[q] = make_float2(s[u][2 * q], s[u][2 * q + 1]);
+          for (int q = 0; q < 4; ++q) p[q] = pair_of<T>(s[u], q);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) d[q] = mul2(d[q], act_slope2(p[q], act));
@@ -1026,7 +1030,7 @@ DzCut cut_dz(int64_t m, int64_t n, int sms) {
   while (bx < 32 && (int64_t)bx * 8 < n) bx *= 2;
   c.block = dim3(bx, 256 / bx);
   c.gx = (int)ceil_div(n, (int64_t)bx * 8);
-  const int64_t most = ceil_div((int64_t)sms * 4, c.gx);
+  const int64_t most = ceil_div((int64_t)sms * 6, c.gx);
   const int64_t step = kDzRows * (int64_t)c.block.y;
   c.rows = (int)round_up(ceil_div(m, most < 256 ? most : 256), step);
   c.gy = (int)ceil_div(m, c.rows);
