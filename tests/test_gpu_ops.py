@@ -505,3 +505,24 @@ def test_refusals(ops):
     for kind, text, call in bad:
         with pytest.raises(kind, match=text):
             call()
+
+
+def test_expired_waits_are_reported(ops):
+    """With a limit that expires at once every role of the product kernel gives
+    up; the call ends, the check reports it once, and the next call is right."""
+    from paper_2608_15438_gb300 import neuroute as nr
+
+    g = gen(2)
+    for m, k, n in ((100, 256, 64), (2000, 512, 512)):  # one CTA a tile, a pair
+        x, w = rows(g, m, k, BF16), rows(g, n, k, BF16, scale=k ** -0.5)
+        want = ops.linear(x, w)
+        ops.check(0)
+        assert nr.lib().nr_ops_wait_limit(-1) == 0
+        try:
+            ops.linear(x, w)
+            with pytest.raises(nr.NRError, match="DEVICE_CHECK"):
+                ops.check(0)
+        finally:
+            assert nr.lib().nr_ops_wait_limit(0) == 0
+        ops.check(0)
+        assert torch.equal(ops.linear(x, w), want)
