@@ -251,9 +251,6 @@ __device__ __forceinline__ void item_of(const Product &P, int item, int &tm, int
   tm = band * kBand + in - tn * height;
 }
 
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
-__device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
-
 template <int CG>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap mb0,
@@ -822,23 +819,6 @@ int64_t parts_bytes(const Cut &c, int64_t rows, int64_t n) {
 }
 
 int64_t wait_limit = kWaitNs;  // nr_ops_wait_limit
-
-// a launch that may begin before the previous one of the call has ended: its
-// kernel waits (grid_wait) before it touches memory
-template <typename... K, typename... A>
-cudaError_t launch(void (*kernel)(K...), unsigned grid, dim3 block, uint32_t smem, cudaStream_t s, bool follows, A &&...a) {
-  cudaLaunchConfig_t c = {};
-  c.gridDim = dim3(grid);
-  c.blockDim = block;
-  c.dynamicSmemBytes = smem;
-  c.stream = s;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  c.attrs = &at;
-  c.numAttrs = follows ? 1 : 0;
-  return cudaLaunchKernelEx(&c, kernel, static_cast<K>(a)...);
-}
 
 // an operand pair, its cut and what becomes of C
 struct Task {

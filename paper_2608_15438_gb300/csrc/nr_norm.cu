@@ -68,6 +68,22 @@ __device__ __forceinline__ int column(int eights, int v, int q, int t, int width
   return eights ? (v * w + t) * 8 + q : (v * 8 + q) * w + t;
 }
 
+// a value if `in`, else 0, in one predicated load
+__device__ __forceinline__ uint32_t load_if32(const void *p, bool in) {
+  uint32_t v;
+  asm("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n mov.b32 %0, 0;\n @p ld.global.nc.b32 %0, [%1];\n}\n"
+      : "=r"(v)
+      : "l"(p), "r"((int)in));
+  return v;
+}
+__device__ __forceinline__ uint16_t load_if16(const void *p, bool in) {
+  uint16_t v;
+  asm("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n mov.b16 %0, 0;\n @p ld.global.nc.b16 %0, [%1];\n}\n"
+      : "=h"(v)
+      : "l"(p), "r"((int)in));
+  return v;
+}
+
 template <int TPR, typename T>
 __device__ __forceinline__ Raw<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, int width = TPR) {
   Raw<T> o = {};
@@ -85,17 +101,14 @@ __device__ __forceinline__ Raw<T> load_raw(const T *row, int eights, bool vec, i
     }
     return o;
   }
-  // loads without branches, so that all are under way at once
+  // predicated loads without branches, so that all are under way at once
+  const int st = eights ? 1 : TPR ? TPR : width;
+  const T *p = row + c;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const int cq = eights ? c + q : c + q * (TPR ? TPR : width), at = min(cq, n - 1);
-    if (sizeof(T) == 4) {
-      const uint32_t u = __ldg(reinterpret_cast<const uint32_t *>(row) + at);
-      o.r[q % (sizeof(T) * 2)] = cq < n ? u : 0u;
-    } else {
-      const uint32_t u = __ldg(reinterpret_cast<const uint16_t *>(row) + at);
-      o.r[q >> 1] |= cq < n ? u << (16 * (q & 1)) : 0u;
-    }
+  for (int q = 0; q < 8; ++q, p += st) {
+    const bool in = c + q * st < n;
+    if (sizeof(T) == 4) o.r[q % (sizeof(T) * 2)] = load_if32(p, in);
+    else o.r[q >> 1] |= (uint32_t)load_if16(p, in) << (16 * (q & 1));
   }
   return o;
 }
@@ -139,11 +152,10 @@ __device__ __forceinline__ void store_row(T *row, int eights, bool vec, int v, i
     if (c < n) store8(row, c, TypeCode<T>::code, 1, 8, o);
     return;
   }
+  const int st = eights ? 1 : TPR ? TPR : width;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const int cq = eights ? c + q : c + q * (TPR ? TPR : width);
-    if (cq < n) row[cq] = from_f32<T>(o[q]);
-  }
+  for (int q = 0; q < 8; ++q)
+    if (c + q * st < n) row[c + q * st] = from_f32<T>(o[q]);
 }
 // eight of the weights (or biases) as a thread's columns need them
 template <int TPR>
@@ -182,8 +194,9 @@ __device__ __forceinline__ void lane_sums(float (&v)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
 }
-// All threads of a block: K sums (a power of two up to 8). A warp halves the
-// values it carries at every exchange, so K sums take K + 5 - log2 K
+// A group of whole warps (`width` threads; the block, or one of several side by
+// side, whose number is `group`): K sums (a power of two up to 8). A warp halves
+// the values it carries at every exchange, so K sums take K + 5 - log2 K
 // exchanges at most; the warps' sums are added in order by every thread. `turn`
 // alternates between two buffers, so that one barrier a call is enough.
 constexpr int kWarpsMax = 16;
@@ -192,8 +205,8 @@ struct BlockSums {
   float part[2][kWarpsMax][K < 4 ? 4 : K];
 };
 template <int K>
-__device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int turn) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+__device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int turn, int t, int width, int group) {
+  const int lane = t & 31, warps = width >> 5, first = group * warps;
   float u[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) u[k] = v[k];
@@ -209,13 +222,14 @@ __device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int t
   }
   for (; o > 0; o >>= 1) u[0] += __shfl_xor_sync(0xffffffffu, u[0], o);
   constexpr int kLanes = 32 / K;  // lanes that hold the same sum
-  if (lane % kLanes == 0) S.part[turn & 1][warp][lane / kLanes] = u[0];
-  __syncthreads();
+  if (lane % kLanes == 0) S.part[turn & 1][first + (t >> 5)][lane / kLanes] = u[0];
+  if (warps > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(group + 1), "r"(width) : "memory");
+  else __syncwarp();
 #pragma unroll
   for (int k = 0; k < K; ++k) v[k] = 0.0f;
   for (int w = 0; w < warps; ++w)
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += S.part[turn & 1][w][k];
+    for (int k = 0; k < K; ++k) v[k] += S.part[turn & 1][first + w][k];
 }
 
 // ------------------------------------------------------------ rows in registers
@@ -455,6 +469,7 @@ __global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const No
     lane_sums<TPR, 2 * R>(G.s);
     G.write(N, i, 0, t, eights, TPR, w);
   }
+  grid_launch();
   if (!N.parts) return;
   float *part = N.parts + (int64_t)blockIdx.x * 2 * N.n;
   for (int g = 0; g < kGroups; ++g) {  // the groups in order
@@ -489,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) 
   int turn = 0;
   for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
     Forward<0, V, R, VEC, T> F;
-    F.statistics(N, i, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++); });
+    F.statistics(N, i, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++, t, width, 0); });
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float2 w[4], b[4];
@@ -501,14 +516,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) 
   }
 }
 
+// Backward: with THREADS 384 blockDim.y groups of blockDim.x threads, R rows each,
+// so that short rows leave few blocks' sums to add; the groups' are added in order.
 template <int V, int R, int THREADS, bool VEC, typename T>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) block_backward_kernel(const Norm N) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ? 2 : 1) block_backward_kernel(const Norm N) {
   __shared__ BlockSums<2 * R> S;
+  extern __shared__ float sums[];  // [2][n], with several groups
   const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
+  const int group = THREADS == 384 ? threadIdx.y : 0, groups = THREADS == 384 ? blockDim.y : 1;
   const bool w_vec = VEC && N.w_vec;
   float2 dw[V][4] = {}, db[V][4] = {};
   int turn = 0;
-  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
+  for (int64_t i = ((int64_t)blockIdx.x * groups + group) * R; i < N.m; i += (int64_t)gridDim.x * groups * R) {
     Backward<0, V, R, VEC, T> G;
     G.load(N, i, t, eights, width);
 #pragma unroll
@@ -517,7 +536,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) block_backwar
       load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
       G.add(v, w, dw[v], db[v]);
     }
-    block_sums<2 * R>(G.s, S, turn++);
+    block_sums<2 * R>(G.s, S, turn++, t, width, group);
     forget();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -526,34 +545,47 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) block_backwar
       G.write(N, i, v, t, eights, width, w);
     }
   }
+  grid_launch();
   if (!N.parts) return;
   float *part = N.parts + (int64_t)blockIdx.x * 2 * N.n;
+  for (int g = 0; g < groups; ++g) {
+    if (group == g) {
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+      for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int c = column<0>(eights, v, q, t, width);
-      if (c >= n) continue;
-      part[c] = q & 1 ? dw[v][q >> 1].y : dw[v][q >> 1].x;
-      part[n + c] = q & 1 ? db[v][q >> 1].y : db[v][q >> 1].x;
+        for (int q = 0; q < 8; ++q) {
+          const int c = column<0>(eights, v, q, t, width);
+          if (c >= n) continue;
+          float a = q & 1 ? dw[v][q >> 1].y : dw[v][q >> 1].x, e = q & 1 ? db[v][q >> 1].y : db[v][q >> 1].x;
+          if (g > 0) {
+            a += sums[c];
+            e += sums[n + c];
+          }
+          float *to = g + 1 < groups ? sums : part;
+          to[c] = a;
+          to[n + c] = e;
+        }
     }
+    if (groups > 1) __syncthreads();
+  }
 }
 
-// dweight, dbias: the blocks' sums, 32 columns a block, eight rows of parts at a time
-__global__ void __launch_bounds__(256)
+// dweight, dbias: the blocks' sums, 32 columns a block, 32 rows of parts at a time
+__global__ void __launch_bounds__(1024)
     norm_params_kernel(const float *parts, int count, int64_t n, void *dweight, void *dbias, int dtype) {
-  __shared__ float sums[8][33];
+  __shared__ float sums[32][33];
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
   const int64_t e = (int64_t)blockIdx.x * 32 + c;  // into [2][n]
+  grid_wait();
   float s = 0.0f;
   if (e < 2 * n) {
 #pragma unroll 8
-    for (int p = r; p < count; p += 8) s += parts[(int64_t)p * 2 * n + e];
+    for (int p = r; p < count; p += 32) s += parts[(int64_t)p * 2 * n + e];
   }
   sums[r][c] = s;
   __syncthreads();
   if (r != 0 || e >= 2 * n) return;
-  for (int q = 1; q < 8; ++q) s += sums[q][c];
+  for (int q = 1; q < 32; ++q) s += sums[q][c];
   store_any(e < n ? dweight : dbias, e < n ? e : e - n, dtype, s);
 }
 
@@ -571,14 +603,14 @@ __global__ void __launch_bounds__(kLongThreads) long_forward_kernel(const Norm N
   const int64_t i = blockIdx.x;
   float s[1] = {0.0f};
   for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) s[0] += long_x(N.x, i, j, dtype);
-  block_sums<1>(s, S, 0);
+  block_sums<1>(s, S, 0, (int)threadIdx.x, kLongThreads, 0);
   const float mean = s[0] / (float)N.n;
   s[0] = 0.0f;
   for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
     const float d = long_x(N.x, i, j, dtype) - mean;
     s[0] = fmaf(d, d, s[0]);
   }
-  block_sums<1>(s, S, 1);
+  block_sums<1>(s, S, 1, (int)threadIdx.x, kLongThreads, 0);
   const float rstd = 1.0f / sqrtf(s[0] / (float)N.n + N.eps);
   for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
     const float w = N.weight ? load_any(N.weight, j, N.w_dtype) : 1.0f, b = N.bias ? load_any(N.bias, j, N.w_dtype) : 0.0f;
@@ -600,7 +632,7 @@ __global__ void __launch_bounds__(kLongThreads) long_dx_kernel(const Norm N, int
     s[0] += g;
     s[1] = fmaf(g, (long_x(N.x, i, j, dtype) - mean) * rstd, s[1]);
   }
-  block_sums<2>(s, S, 0);
+  block_sums<2>(s, S, 0, (int)threadIdx.x, kLongThreads, 0);
   const float m1 = s[0] / (float)N.n, m2 = s[1] / (float)N.n;
   for (int64_t j = threadIdx.x; j < N.n; j += kLongThreads) {
     const float g = load_any(N.dy, i * N.dy_ld + j, dtype) * (N.weight ? load_any(N.weight, j, N.w_dtype) : 1.0f);
@@ -684,27 +716,32 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
 // none is idle. Blocks (tpr 0, v eights a thread, `threads` of them): up to
 // 16384. Longer rows: threads 0.
 struct Shape {
-  int tpr, v, threads;
+  int tpr, v, threads, groups;  // threads a row's group, groups a block
 };
 Shape shape_of(int64_t n, bool vec, bool backward) {
-  if (n <= 256) return {vec && n <= 64 ? 8 : vec && n <= 128 ? 16 : 32, 1, kWarpThreads};
-  if (!backward && n <= 768) return {32, 3, kWarpThreads};
-  if (!backward && n <= 1536) return {32, 6, kWarpThreads};
-  if (n > kLong) return {0, 0, 0};
-  const int v = n <= (backward ? 2048 : 4096) ? 1 : n <= 8192 ? 2 : 4;
-  return {0, v, (int)round_up(ceil_div(n, 8 * v), 32)};
+  if (n <= 256) return {vec && n <= 64 ? 8 : vec && n <= 128 ? 16 : 32, 1, kWarpThreads, 1};
+  if (!backward && n <= 768) return {32, 3, kWarpThreads, 1};
+  if (!backward && n <= 1536) return {32, 6, kWarpThreads, 1};
+  if (n > kLong) return {0, 0, 0, 0};
+  const int v = n > 8192 ? 4 : n > (backward ? 2048 : 4096) ? 2 : 1;
+  const int threads = (int)round_up(ceil_div(n, 8 * v), 32);
+  // groups side by side up to 384 threads: rows of 387 in fp32 leave 304 blocks'
+  // sums instead of 1824 to add (23 us); rows of 1536 ran 15% slower so
+  const int groups = backward && threads <= 128 && v == 1 ? 384 / threads : 1;
+  return {0, v, threads, groups};
 }
 
 // Blocks of a persistent grid: those the registers allow at once, by sizes alone,
 // so that the order of the parameters' sums is fixed.
 int block_count(const Shape &s, int64_t m, bool backward, int sms) {
-  int per_sm, rows;
+  int per_sm, rows = s.groups;
   if (s.tpr) {
     per_sm = s.v == 6 ? 5 : 4;
     rows = kWarpThreads / s.tpr;
+  } else if (backward && s.v == 1) {
+    per_sm = 768 / (s.threads * s.groups);
   } else {
-    per_sm = s.threads <= 256 && s.v == 1 ? 768 / s.threads : (s.v == 4 || backward ? 512 : 1024) / s.threads;
-    rows = 1;
+    per_sm = (!backward && s.v < 4 ? s.threads <= 256 ? 768 : 1024 : 512) / s.threads;
   }
   const int64_t need = ceil_div(m, rows), most = (int64_t)sms * per_sm;
   return (int)(need < most ? need : most);
@@ -734,20 +771,24 @@ cudaError_t backward_typed(const Norm &N, const Shape &s, int blocks, cudaStream
   if (s.tpr == 8) warp_backward_kernel<8, true, T><<<blocks, th, 0, st>>>(N);
   else if (s.tpr == 16) warp_backward_kernel<16, true, T><<<blocks, th, 0, st>>>(N);
   else if (s.tpr) warp_backward_kernel<32, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.v == 1) block_backward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.v == 2) block_backward_kernel<2, block_rows<VEC, T>() / 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1 && s.groups == 1)
+    block_backward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1)
+    block_backward_kernel<1, block_rows<VEC, T>(), 384, VEC, T>
+        <<<blocks, dim3(th, s.groups), (size_t)N.n * 8, st>>>(N);
+  else if (s.v == 2) block_backward_kernel<2, VEC && sizeof(T) == 2 ? 2 : 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
   else block_backward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
   return cudaGetLastError();
 }
 template <typename T>
-cudaError_t launch(const Norm &N, const Shape &s, bool backward, int blocks, cudaStream_t st) {
+cudaError_t launch_typed(const Norm &N, const Shape &s, bool backward, int blocks, cudaStream_t st) {
   if (backward) return N.vec ? backward_typed<true, T>(N, s, blocks, st) : backward_typed<false, T>(N, s, blocks, st);
   return N.vec ? forward_typed<true, T>(N, s, blocks, st) : forward_typed<false, T>(N, s, blocks, st);
 }
 cudaError_t launch_any(const Norm &N, const Shape &s, bool backward, int64_t dtype, int blocks, cudaStream_t st) {
-  if (dtype == NR_F32) return launch<float>(N, s, backward, blocks, st);
-  if (dtype == NR_F16) return launch<__half>(N, s, backward, blocks, st);
-  return launch<__nv_bfloat16>(N, s, backward, blocks, st);
+  if (dtype == NR_F32) return launch_typed<float>(N, s, backward, blocks, st);
+  if (dtype == NR_F16) return launch_typed<__half>(N, s, backward, blocks, st);
+  return launch_typed<__nv_bfloat16>(N, s, backward, blocks, st);
 }
 constexpr int kLongParts = 32;
 
@@ -808,9 +849,8 @@ extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, 
     e = cudaGetLastError();
   }
   if (e == cudaSuccess && N.parts) {
-    norm_params_kernel<<<(unsigned)ceil_div(2 * a->n, 32), 256, 0, s>>>(N.parts, parts, a->n, a->dweight, a->dbias,
-                                                                        (int)a->w_dtype);
-    e = cudaGetLastError();
+    e = launch(norm_params_kernel, (unsigned)ceil_div(2 * a->n, 32), dim3(1024), 0, s, true, N.parts, parts, a->n,
+               a->dweight, a->dbias, (int)a->w_dtype);
   }
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }

@@ -12,6 +12,10 @@
 
 constexpr int kOpsGroup = 32;  // columns that share a checkpoint's scale
 
+// ------------------------------------------------------------ launches that follow one another
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+__device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+
 // ------------------------------------------------------------ element types
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
@@ -276,3 +280,20 @@ constexpr int64_t kOpsMaxRows = ((int64_t)1 << 31) - 1, kOpsMaxCols = ((int64_t)
 int nr_ops_sms(int device);
 // the device's flag that expired waits set (the address, looked up once)
 cudaError_t nr_ops_flag(int device, int **flag);
+
+// a launch that may begin before the previous one of the call has ended: its
+// kernel waits (grid_wait) before it touches memory
+template <typename... K, typename... A>
+cudaError_t launch(void (*kernel)(K...), unsigned grid, dim3 block, uint32_t smem, cudaStream_t s, bool follows, A &&...a) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = block;
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at;
+  c.numAttrs = follows ? 1 : 0;
+  return cudaLaunchKernelEx(&c, kernel, static_cast<K>(a)...);
+}
