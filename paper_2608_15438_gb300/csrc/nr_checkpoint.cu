@@ -17,7 +17,7 @@ __device__ __forceinline__ uint32_t largest(const Eight<T> &o) {
   if (sizeof(T) == 4) {
     uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) top = max(top, o.r[q % (sizeof(T) * 2)] & 0x7fffffffu);
+    for (int q = 0; q < 8; ++q) top = max(top, o.r[q] & 0x7fffffffu);
     return top;
   }
   uint32_t top = o.r[0] & 0x7fff7fffu;
@@ -28,9 +28,11 @@ __device__ __forceinline__ uint32_t largest(const Eight<T> &o) {
 }
 // Threads of a block: x along a row (eight columns each, four threads a group),
 // y over rows; a thread takes kBatch rows at a time, all their loads first.
-template <typename T>
+// VEC: n is a multiple of 8 and the rows take 16-byte accesses.
+template <bool VEC, typename T>
 __global__ void __launch_bounds__(kThreads)
-    write8_kernel(const T *x, int vec, int64_t m, int n, int groups, int64_t x_ld, int8_t *codes, uint8_t *scales) {
+    write8_kernel(const T *x, int64_t m, int n, int groups, int64_t x_ld, int8_t *codes, uint8_t *scales) {
+  const T *end = x + (m - 1) * x_ld + n;
   const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
   const int count = max(0, min(8, n - j));
   const bool in = j < groups * kOpsGroup;
@@ -40,10 +42,11 @@ __global__ void __launch_bounds__(kThreads)
     Eight<T> v[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      v[u] = i0 + u * step < m && count > 0 ? read_eight<T>(x + (i0 + u * step) * x_ld + j, vec, count) : Eight<T>{};
+      v[u] = VEC && count <= 0 ? Eight<T>{} : fetch_eight<T>(x + min(i0 + u * step, m - 1) * x_ld + j, VEC, VEC ? 8 : count, x, end);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int64_t i = i0 + u * step;
+      if (!VEC) settle_eight<T>(v[u], x + min(i, m - 1) * x_ld + j, VEC, count, x, end);
       uint32_t top = largest<T>(v[u]);
       top = max(top, __shfl_xor_sync(lanes, top, 1));
       top = max(top, __shfl_xor_sync(lanes, top, 2));
@@ -58,22 +61,24 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-template <typename T>
+template <bool VEC, typename T>
 __global__ void __launch_bounds__(kThreads)
-    read8_kernel(const int8_t *codes, const uint8_t *scales, int64_t m, int n, int groups, int act, T *y, int vec,
-                 int64_t y_ld) {
-  const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
-  if (j >= n) return;
-  const int count = min(8, n - j);
+    read8_kernel(const int8_t *codes, const uint8_t *scales, int64_t m, int n, int groups, int act, T *y, int64_t y_ld) {
+  const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8, count = max(0, min(8, n - j));
   const int64_t step = (int64_t)gridDim.y * blockDim.y;
+  // the lanes of a warp that share a row, for stores at any address
+  const int lane = (threadIdx.y * blockDim.x + threadIdx.x) & 31, share = min((int)blockDim.x, 32);
+  const unsigned lanes = share == 32 ? 0xffffffffu : ((1u << share) - 1u) << (lane & ~(share - 1));
+  const bool prev = (lane & (share - 1)) != 0, next = (lane & (share - 1)) != share - 1;
+  const int jc = min(j, groups * kOpsGroup - 8);  // lanes past the row load its last eight
   for (int64_t i0 = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; i0 < m; i0 += step * kBatch) {
     uint2 c[kBatch];
     uint32_t s[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int64_t i = min(i0 + u * step, m - 1);
-      c[u] = __ldg(reinterpret_cast<const uint2 *>(codes + i * groups * kOpsGroup + j));
-      s[u] = __ldg(scales + i * groups + (j >> 5));
+      c[u] = __ldg(reinterpret_cast<const uint2 *>(codes + i * groups * kOpsGroup + jc));
+      s[u] = __ldg(scales + i * groups + (jc >> 5));
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -97,7 +102,13 @@ __global__ void __launch_bounds__(kThreads)
         }
       }
       const float v[8] = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
-      store8(y + i * y_ld, j, TypeCode<T>::code, vec, count, v);
+      if (VEC || sizeof(T) == 4) {
+        if (count > 0) store8(y + i * y_ld, j, TypeCode<T>::code, VEC, VEC ? 8 : count, v);
+      } else {
+        const uint4 h = pack8(p, TypeCode<T>::code);
+        const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+        store16x8(y + i * y_ld + j, count, w, prev, next, lanes);
+      }
     }
   }
 }
@@ -129,15 +140,20 @@ extern "C" nr_status nr_checkpoint8_write(const void *x, int dtype, int64_t m, i
   dim3 grid, block;
   cut(m, n, nr_ops_sms(device), grid, block);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int vec = vec_ok(x, x_ld, dtype);
+  const bool vec = n % 8 == 0 && vec_ok(x, x_ld, dtype);
   int8_t *c = static_cast<int8_t *>(codes);
   uint8_t *sc = static_cast<uint8_t *>(scales);
-  if (dtype == NR_F32)
-    write8_kernel<<<grid, block, 0, s>>>(static_cast<const float *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
-  else if (dtype == NR_F16)
-    write8_kernel<<<grid, block, 0, s>>>(static_cast<const __half *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
-  else
-    write8_kernel<<<grid, block, 0, s>>>(static_cast<const __nv_bfloat16 *>(x), vec, m, (int)n, (int)groups, x_ld, c, sc);
+#define NR_WRITE8(T)                                                                                             \
+  if (vec) write8_kernel<true, T><<<grid, block, 0, s>>>(static_cast<const T *>(x), m, (int)n, (int)groups, x_ld, c, sc); \
+  else write8_kernel<false, T><<<grid, block, 0, s>>>(static_cast<const T *>(x), m, (int)n, (int)groups, x_ld, c, sc);
+  if (dtype == NR_F32) {
+    NR_WRITE8(float)
+  } else if (dtype == NR_F16) {
+    NR_WRITE8(__half)
+  } else {
+    NR_WRITE8(__nv_bfloat16)
+  }
+#undef NR_WRITE8
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }
@@ -152,15 +168,20 @@ extern "C" nr_status nr_checkpoint8_read(const void *codes, const void *scales, 
   dim3 grid, block;
   cut(m, n, nr_ops_sms(device), grid, block);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int vec = vec_ok(y, y_ld, dtype);
+  const bool vec = n % 8 == 0 && vec_ok(y, y_ld, dtype);
   const int8_t *c = static_cast<const int8_t *>(codes);
   const uint8_t *sc = static_cast<const uint8_t *>(scales);
-  if (dtype == NR_F32)
-    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<float *>(y), vec, y_ld);
-  else if (dtype == NR_F16)
-    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<__half *>(y), vec, y_ld);
-  else
-    read8_kernel<<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<__nv_bfloat16 *>(y), vec, y_ld);
+#define NR_READ8(T)                                                                                            \
+  if (vec) read8_kernel<true, T><<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<T *>(y), y_ld); \
+  else read8_kernel<false, T><<<grid, block, 0, s>>>(c, sc, m, (int)n, (int)groups, act, static_cast<T *>(y), y_ld);
+  if (dtype == NR_F32) {
+    NR_READ8(float)
+  } else if (dtype == NR_F16) {
+    NR_READ8(__half)
+  } else {
+    NR_READ8(__nv_bfloat16)
+  }
+#undef NR_READ8
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }

@@ -82,11 +82,6 @@ __device__ __forceinline__ void add_raw(float2 (&v)[4], const uint4 &r, int dtyp
   v[0] = add2(v[0], unpack2(r.x, dtype)), v[1] = add2(v[1], unpack2(r.y, dtype));
   v[2] = add2(v[2], unpack2(r.z, dtype)), v[3] = add2(v[3], unpack2(r.w, dtype));
 }
-__device__ __forceinline__ uint4 pack8(const float2 (&v)[4], int dtype) {
-  return make_uint4(pack2(v[0].x, v[0].y, dtype), pack2(v[1].x, v[1].y, dtype), pack2(v[2].x, v[2].y, dtype),
-                    pack2(v[3].x, v[3].y, dtype));
-}
-
 // Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'), row_ok
 // false for rows past the end; called as hold8 is.
 __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, bool row_ok, float2 (&v)[4],
@@ -651,13 +646,14 @@ __global__ void __launch_bounds__(256, 3)
     Eight<T> s[kDzRows];
     float down[kDzRows];
     const int there = VEC ? 8 : count;
+    const void *dy_end = dy + (m - 1) * dy_ld + n, *z_end = static_cast<const T *>(z.p) + (m - 1) * z.ld + n;
 #pragma unroll
-    for (int u = 0; u < kDzRows; ++u) v[u] = read_eight<D>(dy + min(i0 + u * step, i1 - 1) * dy_ld + j, VEC, there);
+    for (int u = 0; u < kDzRows; ++u) v[u] = fetch_eight<D>(dy + min(i0 + u * step, i1 - 1) * dy_ld + j, VEC, there, dy, dy_end);
     if (act != NR_ACT_NONE) {
       if (!z.scale) {
 #pragma unroll
         for (int u = 0; u < kDzRows; ++u)
-          s[u] = read_eight<T>(static_cast<const T *>(z.p) + min(i0 + u * step, i1 - 1) * z.ld + j, VEC, there);
+          s[u] = fetch_eight<T>(static_cast<const T *>(z.p) + min(i0 + u * step, i1 - 1) * z.ld + j, VEC, there, z.p, z_end);
       } else {
 #pragma unroll
         for (int u = 0; u < kDzRows; ++u) {
@@ -672,6 +668,9 @@ __global__ void __launch_bounds__(256, 3)
     for (int u = 0; u < kDzRows; ++u) {
       const int64_t i = i0 + u * step;
       if (i >= i1) break;
+      settle_eight<D>(v[u], dy + i * dy_ld + j, VEC, there, dy, dy_end);
+      if (act != NR_ACT_NONE && !z.scale)
+        settle_eight<T>(s[u], static_cast<const T *>(z.p) + i * z.ld + j, VEC, there, z.p, z_end);
       float2 d[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) d[q] = pair_of<D>(v[u], q);
@@ -725,11 +724,11 @@ __global__ void __launch_bounds__(256) pack_kernel(const Pack K) {
   const int64_t i = e / segs;
   const int j = (int)(e - i * segs) * 8;
   if (i >= K.rows[which]) return;
-  const uint16_t *s = K.s[which] + i * K.s_ld[which] + j;
-  uint32_t v[4] = {};
-#pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (j + q < cols) v[q >> 1] |= (uint32_t)__ldg(s + q) << (16 * (q & 1));
+  const uint16_t *s = K.s[which];
+  const uint16_t *p = s + i * K.s_ld[which] + j, *end = s + (K.rows[which] - 1) * K.s_ld[which] + cols;
+  uint32_t v[8];
+  fetch16x8(p, min(8, cols - j), s, end, v);
+  settle16x8(p, min(8, cols - j), s, end, v);
   *reinterpret_cast<uint4 *>(K.d[which] + i * K.d_ld[which] + j) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 

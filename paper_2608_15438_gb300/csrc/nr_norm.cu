@@ -14,9 +14,10 @@
 // keeps the parameters' sums of its columns in registers over all its rows, and
 // a second kernel adds the blocks' sums in order.
 //
-// A thread's columns: eight consecutive ones at a time where every matrix
-// allows 16-byte accesses (or x is a checkpoint), else single ones a group's width
-// apart, so that a group's accesses stay contiguous. Rows longer than 16384
+// A thread's columns: eight consecutive ones at a time, by 16-byte accesses where
+// every matrix allows them and by shifting pairs of aligned ones where 16-bit rows
+// do not; in fp32 at other addresses single ones a group's width apart, so that a
+// group's accesses stay contiguous. Rows longer than 16384
 // are read again from memory by a block a row (the long_ kernels).
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -48,16 +49,11 @@ struct Norm {
   int64_t dres_ld;
   void *dx;
   int64_t dx_ld;
+  const void *x_end, *dy_end, *dres_end;  // past the matrices' last values
   float *parts;  // [blocks][2][n]: the blocks' sums for dweight, dbias
   int eights;    // a thread's columns come in eights
   int vec;       // and every matrix takes 16-byte accesses
   int w_vec;     // as do weight and bias
-};
-
-// A thread's v-th eight elements of a row as they lie in memory.
-template <typename T>
-struct Raw {
-  uint32_t r[sizeof(T) == 4 ? 8 : 4];
 };
 
 // the column of element q of the thread's v-th eight, of a group of TPR threads
@@ -76,54 +72,32 @@ __device__ __forceinline__ uint32_t load_if32(const void *p, bool in) {
       : "l"(p), "r"((int)in));
   return v;
 }
-__device__ __forceinline__ uint16_t load_if16(const void *p, bool in) {
-  uint16_t v;
-  asm("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n mov.b16 %0, 0;\n @p ld.global.nc.b16 %0, [%1];\n}\n"
-      : "=h"(v)
-      : "l"(p), "r"((int)in));
-  return v;
-}
-
 template <int TPR, typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, int width = TPR) {
-  Raw<T> o = {};
+__device__ __forceinline__ Eight<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, const void *lo, const void *hi,
+                                             int width = TPR) {
   const int c = column<TPR>(eights, v, 0, t, width);
-  if (vec) {  // n is a multiple of 8
-    if (c < n) {
-      const uint4 *p = reinterpret_cast<const uint4 *>(row + c);
-      const uint4 a = __ldg(p);
-      o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
-      if (sizeof(T) == 4) {
-        const uint4 b = __ldg(p + 1);
-        o.r[4 % (sizeof(T) * 2)] = b.x, o.r[5 % (sizeof(T) * 2)] = b.y;
-        o.r[6 % (sizeof(T) * 2)] = b.z, o.r[7 % (sizeof(T) * 2)] = b.w;
-      }
-    }
-    return o;
-  }
+  if (vec) return c < n ? fetch_eight<T>(row + c, true, 8, lo, hi) : Eight<T>{};  // n is a multiple of 8
+  if (sizeof(T) == 2) return fetch_eight<T>(row + c, false, min(8, n - c), lo, hi);
   // predicated loads without branches, so that all are under way at once
+  Eight<T> o;
   const int st = eights ? 1 : TPR ? TPR : width;
   const T *p = row + c;
 #pragma unroll
-  for (int q = 0; q < 8; ++q, p += st) {
-    const bool in = c + q * st < n;
-    if (sizeof(T) == 4) o.r[q % (sizeof(T) * 2)] = load_if32(p, in);
-    else o.r[q >> 1] |= (uint32_t)load_if16(p, in) << (16 * (q & 1));
-  }
+  for (int q = 0; q < 8; ++q, p += st) o.r[q] = load_if32(p, c + q * st < n);
   return o;
 }
-// elements 2 p and 2 p + 1
-template <typename T>
-__device__ __forceinline__ float2 raw_pair(const Raw<T> &o, int p) {
-  if (sizeof(T) == 4)
-    return make_float2(__uint_as_float(o.r[2 * p % (sizeof(T) * 2)]), __uint_as_float(o.r[(2 * p + 1) % (sizeof(T) * 2)]));
-  return unpack2(o.r[p], TypeCode<T>::code);
+template <int TPR, typename T>
+__device__ __forceinline__ void settle_raw(Eight<T> &o, const T *row, bool vec, int v, int t, int n, const void *lo,
+                                           const void *hi, int width = TPR) {
+  if (vec || sizeof(T) == 4) return;
+  const int c = column<TPR>(1, v, 0, t, width);
+  settle_eight<T>(o, row + c, false, min(8, n - c), lo, hi);
 }
 // x, which may be a checkpoint: then the codes as numbers of T, exactly, and
 // their scale
 template <int TPR, typename T>
-__device__ __forceinline__ Raw<T> load_held(const Rows &x, int64_t i, int v, int t, int n, float &scale, int width = TPR) {
-  Raw<T> o = {};
+__device__ __forceinline__ Eight<T> load_held(const Rows &x, int64_t i, int v, int t, int n, float &scale, int width = TPR) {
+  Eight<T> o = {};
   scale = 1.0f;
   const int c = column<TPR>(1, v, 0, t, width);
   if (c < n) {
@@ -135,8 +109,8 @@ __device__ __forceinline__ Raw<T> load_held(const Rows &x, int64_t i, int v, int
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (sizeof(T) == 4) {
-        o.r[2 * q % (sizeof(T) * 2)] = __float_as_uint(p[q].x);
-        o.r[(2 * q + 1) % (sizeof(T) * 2)] = __float_as_uint(p[q].y);
+        o.r[2 * q] = __float_as_uint(p[q].x);
+        o.r[2 * q + 1] = __float_as_uint(p[q].y);
       } else {
         o.r[q] = pack2(p[q].x, p[q].y, TypeCode<T>::code);
       }
@@ -150,6 +124,15 @@ __device__ __forceinline__ void store_row(T *row, int eights, bool vec, int v, i
   const int c = column<TPR>(eights, v, 0, t, width);
   if (vec) {
     if (c < n) store8(row, c, TypeCode<T>::code, 1, 8, o);
+    return;
+  }
+  if (sizeof(T) == 2) {  // a group's lanes of a warp walk a row in step
+    constexpr int kShare = TPR > 0 && TPR < 32 ? TPR : 32;
+    const uint4 h = pack8(p, TypeCode<T>::code);
+    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+    const int lane = threadIdx.x & 31, at = lane & (kShare - 1);
+    const unsigned lanes = kShare == 32 ? 0xffffffffu : ((1u << (kShare & 31)) - 1u) << (lane & ~(kShare - 1));
+    store16x8(row + c, max(0, min(8, n - c)), w, at > 0, at < kShare - 1, lanes);
     return;
   }
   const int st = eights ? 1 : TPR ? TPR : width;
@@ -180,7 +163,7 @@ __device__ __forceinline__ void load_w(const void *p, int dtype, float none, int
 // reuse after it: the registers buy more rows in flight.
 __device__ __forceinline__ void forget() { asm volatile("" ::: "memory"); }
 template <typename T>
-__device__ __forceinline__ void forget(Raw<T> &o) {
+__device__ __forceinline__ void forget(Eight<T> &o) {
 #pragma unroll
   for (int k = 0; k < (sizeof(T) == 4 ? 8 : 4); ++k) asm volatile("" : "+r"(o.r[k]));
 }
@@ -245,20 +228,22 @@ struct Forward {
   __device__ __forceinline__ void statistics(const Norm &N, int64_t i, int t, int eights, int width, Sums sums) {
     const int n = (int)N.n;
     const float inv = 1.0f / (float)n;
-    Raw<T> raw[R][V];
+    Eight<T> raw[R][V];
     if (!N.x.scale) {
       const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, n, width) : Raw<T>{};
+          raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, n, N.x.p, N.x_end, width) : Eight<T>{};
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+          if (i + r < N.m) settle_raw<TPR, T>(raw[r][v], p + r * N.x.ld, VEC, v, t, n, N.x.p, N.x_end, width);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) x[r][v][q] = raw_pair(raw[r][v], q);
+          for (int q = 0; q < 4; ++q) x[r][v][q] = pair_of<T>(raw[r][v], q);
+        }
     } else {
       float scale[R][V];
 #pragma unroll
@@ -270,7 +255,7 @@ struct Forward {
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) x[r][v][q] = mul2(raw_pair(raw[r][v], q), both(scale[r][v]));
+          for (int q = 0; q < 4; ++q) x[r][v][q] = mul2(pair_of<T>(raw[r][v], q), both(scale[r][v]));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -335,7 +320,7 @@ struct Forward {
 // converted twice.
 template <int TPR, int V, int R, bool VEC, typename T>
 struct Backward {
-  Raw<T> x[R][V], dy[R][V];
+  Eight<T> x[R][V], dy[R][V];
   float scale[R][V], shift[R], rstd[R];  // xh = x scale + shift
   float s[2 * R];                        // sum g, sum g xh of the thread's columns, then of the rows
 
@@ -348,7 +333,7 @@ struct Backward {
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        dy[r][v] = i + r < N.m ? load_raw<TPR, T>(pd + r * N.dy_ld, eights, VEC, v, t, n, width) : Raw<T>{};
+        dy[r][v] = i + r < N.m ? load_raw<TPR, T>(pd + r * N.dy_ld, eights, VEC, v, t, n, N.dy, N.dy_end, width) : Eight<T>{};
     if (N.x.scale) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
@@ -359,8 +344,18 @@ struct Backward {
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          x[r][v] = i + r < N.m ? load_raw<TPR, T>(px + r * N.x.ld, eights, VEC, v, t, n, width) : Raw<T>{};
+          x[r][v] = i + r < N.m ? load_raw<TPR, T>(px + r * N.x.ld, eights, VEC, v, t, n, N.x.p, N.x_end, width) : Eight<T>{};
           scale[r][v] = 1.0f;
+        }
+    }
+    if (!VEC) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (i + r >= N.m) break;
+          settle_raw<TPR, T>(dy[r][v], pd + r * N.dy_ld, VEC, v, t, n, N.dy, N.dy_end, width);
+          if (!N.x.scale) settle_raw<TPR, T>(x[r][v], px + r * N.x.ld, VEC, v, t, n, N.x.p, N.x_end, width);
         }
     }
 #pragma unroll
@@ -383,8 +378,8 @@ struct Backward {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         // dy is zero past the row's end, and xh finite where the row is
-        const float2 d = raw_pair(dy[r][v], q), g = mul2(d, w[q]);
-        const float2 xh = fma2(raw_pair(x[r][v], q), both(scale[r][v]), both(shift[r]));
+        const float2 d = pair_of<T>(dy[r][v], q), g = mul2(d, w[q]);
+        const float2 xh = fma2(pair_of<T>(x[r][v], q), both(scale[r][v]), both(shift[r]));
         s1 = add2(s1, g);
         s2 = fma2(g, xh, s2);
         db[q] = add2(db[q], d);
@@ -408,13 +403,14 @@ struct Backward {
       float2 o[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const float2 xh = fma2(raw_pair(x[r][v], q), both(scale[r][v]), both(shift[r]));
-        o[q] = fma2(xh, m2, fma2(mul2(raw_pair(dy[r][v], q), w[q]), both(rstd[r]), m1));
+        const float2 xh = fma2(pair_of<T>(x[r][v], q), both(scale[r][v]), both(shift[r]));
+        o[q] = fma2(xh, m2, fma2(mul2(pair_of<T>(dy[r][v], q), w[q]), both(rstd[r]), m1));
       }
       if (N.dres) {
-        const Raw<T> rr = load_raw<TPR, T>(res + r * N.dres_ld, eights, VEC, v, t, (int)N.n, width);
+        Eight<T> rr = load_raw<TPR, T>(res + r * N.dres_ld, eights, VEC, v, t, (int)N.n, N.dres, N.dres_end, width);
+        settle_raw<TPR, T>(rr, res + r * N.dres_ld, VEC, v, t, (int)N.n, N.dres, N.dres_end, width);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = add2(o[q], raw_pair(rr, q));
+        for (int q = 0; q < 4; ++q) o[q] = add2(o[q], pair_of<T>(rr, q));
       }
       store_row<TPR, T>(dx + r * N.dx_ld, eights, VEC, v, t, (int)N.n, o, width);
     }
@@ -704,13 +700,17 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
   else
     vec = vec && vec_ok(a->y, a->y_ld, dt);
   N.vec = vec;
-  N.eights = vec || a->x_scale;
+  N.eights = vec || a->x_scale || dt != NR_F32;
+  const int64_t e = (int64_t)type_bytes(dt);
+  N.x_end = static_cast<const char *>(a->x) + ((a->m - 1) * a->x_ld + a->n) * e;
+  N.dy_end = static_cast<const char *>(a->dy) + ((a->m - 1) * a->dy_ld + a->n) * e;
+  N.dres_end = static_cast<const char *>(a->residual_grad) + ((a->m - 1) * a->residual_grad_ld + a->n) * e;
   N.w_vec = N.eights && a->n % 8 == 0 && vec_ok(a->weight, 8, a->w_dtype) && vec_ok(a->bias, 8, a->w_dtype);
   return N;
 }
 
 // How a row is held. Warps (tpr lanes a row, v eights a thread): forward up to
-// 1536 columns, where a row's sums cost five exchanges and no barrier;
+// 1536 columns of aligned rows, where a row's sums cost five exchanges and no barrier;
 // backward up to 256, as the parameters' sums are 16 registers an eight and
 // leave too few rows in flight beyond. Fewer lanes take rows of 64 and 128, so that
 // none is idle. Blocks (tpr 0, v eights a thread, `threads` of them): up to
@@ -719,9 +719,9 @@ struct Shape {
   int tpr, v, threads, groups;  // threads a row's group, groups a block
 };
 Shape shape_of(int64_t n, bool vec, bool backward) {
-  if (n <= 256) return {vec && n <= 64 ? 8 : vec && n <= 128 ? 16 : 32, 1, kWarpThreads, 1};
-  if (!backward && n <= 768) return {32, 3, kWarpThreads, 1};
-  if (!backward && n <= 1536) return {32, 6, kWarpThreads, 1};
+  if (n <= 256) return {n <= 64 ? 8 : n <= 128 ? 16 : 32, 1, kWarpThreads, 1};
+  if (!backward && vec && n <= 768) return {32, 3, kWarpThreads, 1};
+  if (!backward && vec && n <= 1536) return {32, 6, kWarpThreads, 1};
   if (n > kLong) return {0, 0, 0, 0};
   const int v = n > 8192 ? 4 : n > (backward ? 2048 : 4096) ? 2 : 1;
   const int threads = (int)round_up(ceil_div(n, 8 * v), 32);
@@ -733,7 +733,7 @@ Shape shape_of(int64_t n, bool vec, bool backward) {
 
 // Blocks of a persistent grid: those the registers allow at once, by sizes alone,
 // so that the order of the parameters' sums is fixed.
-int block_count(const Shape &s, int64_t m, bool backward, int sms) {
+int block_count(const Shape &s, int64_t m, bool backward, bool vec, int sms) {
   int per_sm, rows = s.groups;
   if (s.tpr) {
     per_sm = s.v == 6 ? 5 : 4;
@@ -741,7 +741,7 @@ int block_count(const Shape &s, int64_t m, bool backward, int sms) {
   } else if (backward && s.v == 1) {
     per_sm = 768 / (s.threads * s.groups);
   } else {
-    per_sm = (!backward && s.v < 4 ? s.threads <= 256 ? 768 : 1024 : 512) / s.threads;
+    per_sm = (!backward && s.v < 4 ? s.threads <= 256 ? 768 : 1024 : backward && s.v == 2 && !vec ? 580 : 512) / s.threads;
   }
   const int64_t need = ceil_div(m, rows), most = (int64_t)sms * per_sm;
   return (int)(need < most ? need : most);
@@ -754,11 +754,11 @@ constexpr int block_rows() { return VEC && sizeof(T) == 2 ? 4 : 2; }
 template <bool VEC, typename T>
 cudaError_t forward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
   const int th = s.threads;
-  if (s.tpr == 8) warp_forward_kernel<8, 1, true, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr == 16) warp_forward_kernel<16, 1, true, T><<<blocks, th, 0, st>>>(N);
+  if (s.tpr == 8) warp_forward_kernel<8, 1, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_forward_kernel<16, 1, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.tpr && s.v == 1) warp_forward_kernel<32, 1, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr && s.v == 3) warp_forward_kernel<32, 3, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr) warp_forward_kernel<32, 6, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr && s.v == 3) warp_forward_kernel<32, 3, true, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr) warp_forward_kernel<32, 6, true, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1 && th <= 256) block_forward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1) block_forward_kernel<1, 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 2) block_forward_kernel<2, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
@@ -768,8 +768,8 @@ cudaError_t forward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_
 template <bool VEC, typename T>
 cudaError_t backward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
   const int th = s.threads;
-  if (s.tpr == 8) warp_backward_kernel<8, true, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr == 16) warp_backward_kernel<16, true, T><<<blocks, th, 0, st>>>(N);
+  if (s.tpr == 8) warp_backward_kernel<8, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_backward_kernel<16, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.tpr) warp_backward_kernel<32, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1 && s.groups == 1)
     block_backward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
@@ -804,7 +804,7 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
   const Shape sh = shape_of(a->n, N.vec, false);
   cudaError_t e;
   if (sh.threads) {
-    e = launch_any(N, sh, false, a->dtype, block_count(sh, a->m, false, nr_ops_sms(device)), s);
+    e = launch_any(N, sh, false, a->dtype, block_count(sh, a->m, false, N.vec, nr_ops_sms(device)), s);
   } else {
     long_forward_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);
     e = cudaGetLastError();
@@ -815,8 +815,9 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
 extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int device) {
   if (!valid(a, true)) return -1;
   if (a->m == 0 || !a->dweight) return 0;
-  const Shape sh = shape_of(a->n, norm_of(a, true).vec, true);
-  const int64_t blocks = sh.threads ? block_count(sh, a->m, true, nr_ops_sms(device)) : kLongParts;
+  const bool vec = norm_of(a, true).vec;
+  const Shape sh = shape_of(a->n, vec, true);
+  const int64_t blocks = sh.threads ? block_count(sh, a->m, true, vec, nr_ops_sms(device)) : kLongParts;
   return round_up(blocks * 2 * a->n * 4, 256);
 }
 
@@ -840,7 +841,7 @@ extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, 
   const Shape sh = shape_of(a->n, N.vec, true);
   int parts = kLongParts;
   if (sh.threads) {
-    parts = block_count(sh, a->m, true, nr_ops_sms(device));
+    parts = block_count(sh, a->m, true, N.vec, nr_ops_sms(device));
     e = launch_any(N, sh, true, a->dtype, parts, s);
   } else {
     long_dx_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);

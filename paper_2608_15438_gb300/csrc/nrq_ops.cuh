@@ -103,36 +103,116 @@ __device__ __forceinline__ void store8(void *p, int64_t e, int dtype, int vec, i
     if (q < count) store_any(p, e + q, dtype, v[q]);
 }
 
-// eight values of a row as they lie in memory (vec: 16-byte accesses)
+// ------------------------------------------------------------ rows at any 2-byte address
+// Sixteen halves in eight words, from half `by` (0 to 8) on: eight of them.
+__device__ __forceinline__ void shift_halves(uint32_t (&w)[8], int by, uint32_t (&o)[4]) {
+  if (by & 8) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = w[k + 4];
+  }
+#pragma unroll
+  for (int k = 0; k < 6; ++k) w[k] = by & 4 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) w[k] = by & 2 ? w[k + 1] : w[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = __funnelshift_r(w[k], w[k + 1], by & 1 ? 16 : 0);
+}
+// Eight 16-bit values from p on, of which `count` are there: the two aligned
+// 16-byte blocks they lie in (fetch), later shifted into place with zeros after the
+// last (settle), so that many fetches are under way at once. A block that
+// reaches out of the matrix [lo, hi) is not read; the few values at the matrix's
+// first and last bytes that need it are read one by one.
+__device__ __forceinline__ uint4 load_if128(const void *p, bool in) {
+  uint4 v;
+  asm("{\n .reg .pred p;\n setp.ne.b32 p, %5, 0;\n mov.b32 %0, 0;\n mov.b32 %1, 0;\n mov.b32 %2, 0;\n mov.b32 %3, 0;\n"
+      " @p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n}\n"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p), "r"((int)in));
+  return v;
+}
+__device__ __forceinline__ void fetch16x8(const void *p, int count, const void *lo, const void *hi, uint32_t (&w)[8]) {
+  const char *a = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  const uint4 x = load_if128(a, count > 0 && a >= lo && a + 16 <= hi), y = load_if128(a + 16, count > 0 && a + 32 <= hi);
+  w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
+}
+__device__ __forceinline__ void settle16x8(const void *p, int count, const void *lo, const void *hi, uint32_t (&w)[8]) {
+  const char *a = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  const int s = (int)(reinterpret_cast<uintptr_t>(p) & 15) >> 1;
+  uint32_t o[4];
+  if (count > 0 && (a < lo || a + 16 + (s + count > 8 ? 16 : 0) > hi)) {
+    o[0] = o[1] = o[2] = o[3] = 0u;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q < count) o[q >> 1] |= (uint32_t)__ldg(static_cast<const uint16_t *>(p) + q) << (16 * (q & 1));
+  } else {
+    shift_halves(w, s, o);
+    if (count < 8) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = count >= 2 * k + 2 ? o[k] : count == 2 * k + 1 ? o[k] & 0xffffu : 0u;
+    }
+  }
+  w[0] = o[0], w[1] = o[1], w[2] = o[2], w[3] = o[3];
+}
+// Stores eight 16-bit values from p on, of which `count` are there. The lanes of
+// `lanes` call it together, each eight values after its predecessor's, so that an
+// aligned 16-byte block is a lane's first values after its predecessor's last,
+// and all but the ends are whole blocks. prev, next: the neighbouring lane
+// belongs to the row.
+__device__ __forceinline__ void store16x8(void *p, int count, const uint32_t (&v)[4], bool prev, bool next, unsigned lanes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  const int s = (int)(at & 15) >> 1, head = 8 - s;  // values before the next block
+  uint32_t w[8], o[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    w[k] = __shfl_up_sync(lanes, v[k], 1);
+    w[k + 4] = v[k];
+  }
+  shift_halves(w, head, o);
+  const bool block = (prev || s == 0) && count >= head;
+  if (block) *reinterpret_cast<uint4 *>(at - 2 * (uintptr_t)s) = make_uint4(o[0], o[1], o[2], o[3]);
+  const bool tail = s != 0 && !(next && count - 8 >= head);  // no successor writes this lane's last values
+  if (!block || tail) {
+    uint16_t *d = static_cast<uint16_t *>(p);
+    const int from = block ? head : 0, to = tail ? 8 : head;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q >= from && q < to && q < count) d[q] = (uint16_t)(v[q >> 1] >> (16 * (q & 1)));
+  }
+}
+
+// Eight consecutive values of a row as they lie in memory: fetched, then settled
+// (vec: by aligned 16-byte accesses, which leaves nothing to settle).
 template <typename T>
 struct Eight {
-  uint32_t r[sizeof(T) == 4 ? 8 : 4];
+  uint32_t r[8];
 };
 template <typename T>
-__device__ __forceinline__ Eight<T> read_eight(const T *p, bool vec, int count) {
+__device__ __forceinline__ Eight<T> fetch_eight(const T *p, bool vec, int count, const void *lo, const void *hi) {
   Eight<T> o = {};
   if (vec && count == 8) {
     const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
     o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
     if (sizeof(T) == 4) {
       const uint4 b = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
-      o.r[4 % (sizeof(T) * 2)] = b.x, o.r[5 % (sizeof(T) * 2)] = b.y;
-      o.r[6 % (sizeof(T) * 2)] = b.z, o.r[7 % (sizeof(T) * 2)] = b.w;
+      o.r[4] = b.x, o.r[5] = b.y, o.r[6] = b.z, o.r[7] = b.w;
     }
-    return o;
-  }
+  } else if (sizeof(T) == 4) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (q < count) {
-      if (sizeof(T) == 4) o.r[q % (sizeof(T) * 2)] = __ldg(reinterpret_cast<const uint32_t *>(p) + q);
-      else o.r[q >> 1] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + q) << (16 * (q & 1));
-    }
+    for (int q = 0; q < 8; ++q)
+      if (q < count) o.r[q] = __ldg(reinterpret_cast<const uint32_t *>(p) + q);
+  } else {
+    fetch16x8(p, count, lo, hi, o.r);
+  }
   return o;
+}
+template <typename T>
+__device__ __forceinline__ void settle_eight(Eight<T> &o, const T *p, bool vec, int count, const void *lo, const void *hi) {
+  if (sizeof(T) == 2 && !(vec && count == 8)) settle16x8(p, count, lo, hi, o.r);
 }
 template <typename T>
 __device__ __forceinline__ float2 pair_of(const Eight<T> &o, int p) {
   if (sizeof(T) == 4)
-    return make_float2(__uint_as_float(o.r[2 * p % (sizeof(T) * 2)]), __uint_as_float(o.r[(2 * p + 1) % (sizeof(T) * 2)]));
+    return make_float2(__uint_as_float(o.r[2 * p]), __uint_as_float(o.r[2 * p + 1]));
   return unpack2(o.r[p], TypeCode<T>::code);
 }
 
@@ -156,6 +236,11 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return from_bits2(d);
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+__device__ __forceinline__ uint4 pack8(const float2 (&v)[4], int dtype) {
+  return make_uint4(pack2(v[0].x, v[0].y, dtype), pack2(v[1].x, v[1].y, dtype), pack2(v[2].x, v[2].y, dtype),
+                    pack2(v[3].x, v[3].y, dtype));
+}
 
 // ------------------------------------------------------------ activations
 __device__ __forceinline__ float exp2_approx(float v) {
