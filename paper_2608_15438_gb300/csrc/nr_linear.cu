@@ -45,7 +45,7 @@ namespace {
 struct Epilogue {
   const void *bias;
   int bias_dtype, act;
-  const void *residual;  // of type dtype
+  const void *residual, *residual_end;  // of type dtype; past its last value
   int64_t residual_ld;
   void *y;
   int64_t y_ld;
@@ -145,11 +145,31 @@ __device__ __forceinline__ void stage_read(const float *stage, int lane, int u, 
   v[2] = make_float2(hi.x, hi.y), v[3] = make_float2(hi.z, hi.w);
 }
 
-// A whole block (32 rows and columns there, every matrix in vectors, y 16-bit) from
-// row i, column j of the thread's eight: no bounds, one test a step for all rows.
+// eight 16-bit values of a row: the four threads of 32 columns together
+template <bool VEC>
+__device__ __forceinline__ void store_block(uint16_t *p, int lane, const float2 (&v)[4], int dtype) {
+  const uint4 o = pack8(v, dtype);
+  if (VEC) {
+    *reinterpret_cast<uint4 *>(p) = o;
+  } else {
+    const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+    store16x8(p, 8, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
+  }
+}
+
+// A whole block (32 rows and columns there, y 16-bit) from row i, column j of the
+// thread's eight: no bounds, one test a step for all rows. VEC: every matrix takes
+// 16-byte accesses, and res holds the residual, loaded ahead.
+template <bool VEC>
 __device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j, const float *stage, int lane,
                                              const float2 (&b)[4], const uint4 (&res)[4]) {
   float2 v[4][4];
+  uint32_t far[4][8];
+  const uint16_t *pr = static_cast<const uint16_t *>(E.residual) + i * E.residual_ld + j;
+  if (!VEC && E.residual) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) fetch16x8(pr + 8 * u * E.residual_ld, 8, E.residual, E.residual_end, far[u]);
+  }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     stage_read(stage, lane, u, v[u]);
@@ -163,7 +183,7 @@ __device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j
     } else {
       uint16_t *z = static_cast<uint16_t *>(E.z) + i * E.z_ld + j;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4 *>(z + 8 * u * E.z_ld) = pack8(v[u], E.dtype);
+      for (int u = 0; u < 4; ++u) store_block<VEC>(z + 8 * u * E.z_ld, lane, v[u], E.dtype);
     }
   }
 #define NR_BLOCK_ACT(A)                                  \
@@ -179,11 +199,18 @@ __device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j
 #undef NR_BLOCK_ACT
   if (E.residual) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) add_raw(v[u], res[u], E.dtype);
+    for (int u = 0; u < 4; ++u) {
+      if (VEC) {
+        add_raw(v[u], res[u], E.dtype);
+      } else {
+        settle16x8(pr + 8 * u * E.residual_ld, 8, E.residual, E.residual_end, far[u]);
+        add_raw(v[u], make_uint4(far[u][0], far[u][1], far[u][2], far[u][3]), E.dtype);
+      }
+    }
   }
   uint16_t *y = static_cast<uint16_t *>(E.y) + i * E.y_ld + j;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4 *>(y + 8 * u * E.y_ld) = pack8(v[u], E.dtype);
+  for (int u = 0; u < 4; ++u) store_block<VEC>(y + 8 * u * E.y_ld, lane, v[u], E.dtype);
 }
 
 // ------------------------------------------------------------ products on tensor cores
@@ -407,12 +434,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       const int n = (int)E.n;
       const int64_t rows = P.rows;
       const bool partial = P.splits > 1;
-      const bool vectors = E.y_vec && E.y_dtype != NR_F32 && (!E.z || E.z_scale || E.z_vec) &&
-                           (!E.residual || E.residual_vec) && !partial;
       int tm, tn, part;
       item_of(P, second ? item - J.items0 : item, tm, tn, part);
       const uint32_t a = it & 1u;
       const int64_t i0 = ((int64_t)tm * CG + rank) * kRows + lg * 32;
+      const bool blocks = E.y_dtype != NR_F32 && !partial && i0 + 32 <= rows;
+      const bool vectors = E.y_vec && (!E.z || E.z_scale || E.z_vec) && (!E.residual || E.residual_vec);
       // the two warps of a lane quarter take its chunks of 32 columns in turn
       const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < rows ? min(n, (tn + 1) * P.nt) : 0;
       if (__all_sync(0xffffffffu, tc::bar_wait(tc::smem_u32(&B.accfull[a]), (it >> 1) & 1u, abort, limit)) == 0) break;
@@ -420,11 +447,11 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       const uint32_t acc = tmem + lane_base + a * (uint32_t)J.nt - (uint32_t)(tn * P.nt);
       for (int c = c0; c < c1; c += 64) {
         uint32_t v[32];
-        __syncwarp();  // the block's previous readers are done
+        __syncwarp();
         tc::ld32(acc + (uint32_t)c, v);
         const int j = c + seg * 8;
-        const bool whole = vectors && c + 32 <= n && i0 + 32 <= rows;
-        // meanwhile, what the read-back needs
+        const bool whole = blocks && c + 32 <= n;
+        // what the read-back needs, while the sums arrive
         float2 b[4];
         uint4 res[4];
         if (E.bias) {
@@ -433,16 +460,19 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int q = 0; q < 4; ++q) b[q] = both(0.0f);
         }
-        if (E.residual && whole) {
+        if (E.residual && whole && vectors) {
           const uint16_t *p = static_cast<const uint16_t *>(E.residual) + (i0 + r8) * E.residual_ld + j;
 #pragma unroll
           for (int u = 0; u < 4; ++u) res[u] = __ldg(reinterpret_cast<const uint4 *>(p + 8 * u * E.residual_ld));
         }
-        tc::wait_ld();
+        tc::wait_ld(v);
+        __syncwarp();  // the block's previous readers are done
         stage_write(stage, lane, v);
         __syncwarp();
-        if (whole) {
-          finish_block(E, i0 + r8, j, stage, lane, b, res);
+        if (whole && vectors) {
+          finish_block<true>(E, i0 + r8, j, stage, lane, b, res);
+        } else if (whole) {
+          finish_block<false>(E, i0 + r8, j, stage, lane, b, res);
         } else {
 #pragma unroll 1
           for (int u = 0; u < 4; ++u) {
@@ -1099,6 +1129,7 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
   E.act = (int)a->act;
   E.residual = a->residual;
   E.residual_ld = a->residual_ld;
+  E.residual_end = static_cast<const uint16_t *>(a->residual) + (a->m - 1) * a->residual_ld + a->n;
   E.y = a->y;
   E.y_ld = a->y_ld;
   E.z = a->z;
