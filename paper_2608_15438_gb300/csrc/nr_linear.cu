@@ -264,13 +264,23 @@ __device__ __forceinline__ int item_at(int turn, int slot, int slots) {
 // tiles in flight share their slices of A and B in L2.
 __device__ __forceinline__ void item_of(const Product &P, int item, int &tm, int &tn, int &part) {
   const int tiles = P.tiles_m * P.tiles_n;
-  part = item / tiles;
+  part = P.splits > 1 ? item / tiles : 0;
   const int t = item - part * tiles;
   constexpr int kBand = 8;
   const int band = t / (kBand * P.tiles_n), in = t - band * kBand * P.tiles_n;
   const int height = min(kBand, P.tiles_m - band * kBand);
   tn = in / height;
   tm = band * kBand + in - tn * height;
+}
+
+// A part's slices. Splits are rare: the divisions, hundreds of cycles between
+// two tiles' MMAs, are left out without them.
+__device__ __forceinline__ void slices_of(const Product &P, int part, int &s0, int &s1) {
+  s0 = 0, s1 = P.slices;
+  if (P.splits > 1) {  // slices and parts: at most 2^25 and 32
+    s0 = P.slices / P.splits * part + min(part, P.slices % P.splits);
+    s1 = s0 + P.slices / P.splits + (part < P.slices % P.splits ? 1 : 0);
+  }
 }
 
 template <int CG>
@@ -331,7 +341,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
           int tm, tn, part;
           item_of(P, item - from, tm, tn, part);
           const int i0 = (tm * CG + (int)rank) * kRows, j0 = tn * P.nt + (int)rank * nb;
-          const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
+          int s0, s1;
+          slices_of(P, part, s0, s1);
           for (int s = s0; s < s1; ++s) {
             if (!tc::bar_wait(tc::smem_u32(&B.empty[st]), phase, abort, limit)) {
               ok = false;
@@ -378,9 +389,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         for (; ok; ++turn) {
           const int item = item_at(turn, slot, slots);
           if (item >= to) break;
-          int tm, tn, part;
-          item_of(P, item - from, tm, tn, part);
-          const int s0 = (int)((int64_t)P.slices * part / P.splits), s1 = (int)((int64_t)P.slices * (part + 1) / P.splits);
+          int s0, s1;
+          slices_of(P, P.splits > 1 ? (item - from) / (P.tiles_m * P.tiles_n) : 0, s0, s1);
           const uint32_t a = it & 1u, d = tmem + a * (uint32_t)J.nt;
           if (!tc::bar_wait(tc::smem_u32(&B.accempty[a]), ((it >> 1) & 1u) ^ 1u, abort, limit) ||
               !tc::bar_wait(tc::smem_u32(&B.full[st]), phase, abort, limit)) {
@@ -442,6 +452,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       const bool vectors = E.y_vec && (!E.z || E.z_scale || E.z_vec) && (!E.residual || E.residual_vec);
       // the two warps of a lane quarter take its chunks of 32 columns in turn
       const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < rows ? min(n, (tn + 1) * P.nt) : 0;
+      if (E.residual && blocks) {  // the residual's way from memory, while the sums are made
+        const uint16_t *p = static_cast<const uint16_t *>(E.residual) + (i0 + lane) * E.residual_ld;
+        for (int c = c0; c < c1; c += 64) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p + c));
+      }
       if (__all_sync(0xffffffffu, tc::bar_wait(tc::smem_u32(&B.accfull[a]), (it >> 1) & 1u, abort, limit)) == 0) break;
       tc::fence_after();
       const uint32_t acc = tmem + lane_base + a * (uint32_t)J.nt - (uint32_t)(tn * P.nt);
