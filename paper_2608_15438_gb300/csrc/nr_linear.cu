@@ -529,7 +529,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 // What is left after the products, in one launch: block ranges add the parts'
 // sums of a split product in order and finish them (a thread eight columns,
 // padded to whole groups of 32), and the rows of column sums that dz_kernel
-// left into dbias (32 columns a block, eight rows at a time).
+// left into dbias (eight columns a block, 32 rows at a time).
 struct Finish {
   Product p[2];
   int blocks[2];  // of each product; 0: not split
@@ -540,7 +540,7 @@ struct Finish {
   int dbias_dtype;
 };
 __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Finish F) {
-  __shared__ float sums[8][33];
+  __shared__ float sums[32][9];
   grid_wait();
   int block = (int)blockIdx.x;
   const int which = block < F.blocks[0] ? 0 : 1;
@@ -568,17 +568,17 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
     return;
   }
   block -= F.blocks[1];
-  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t j = (int64_t)block * 32 + c;
+  const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+  const int64_t j = (int64_t)block * 8 + c;
   float s = 0.0f;
   if (j < F.sums_n) {
 #pragma unroll 8
-    for (int p = r; p < F.sums_rows; p += 8) s += F.sums[(int64_t)p * F.sums_n + j];
+    for (int p = r; p < F.sums_rows; p += 32) s += F.sums[(int64_t)p * F.sums_n + j];
   }
   sums[r][c] = s;
   __syncthreads();
   if (r != 0 || j >= F.sums_n) return;
-  for (int q = 1; q < 8; ++q) s += sums[q][c];
+  for (int q = 1; q < 32; ++q) s += sums[q][c];
   store_any(F.dbias, j, F.dbias_dtype, s);
 }
 
@@ -595,6 +595,7 @@ __global__ void __launch_bounds__(kRowsThreads)
   const int kp = warp % ks;
   const int64_t j0 = ((int64_t)blockIdx.x * (kRowsThreads / 32 / ks) + warp / ks) * NR;
   float acc[MR][NR] = {};
+  float2 acc2[MR][NR] = {};
   const T *xr[MR], *wr[NR];
 #pragma unroll
   for (int r = 0; r < MR; ++r) xr[r] = x + (int64_t)min(r, m - 1) * x_ld;
@@ -603,27 +604,39 @@ __global__ void __launch_bounds__(kRowsThreads)
   if (j0 < n) {
     if (vec) {
       const int64_t k8 = k / 8;
-#pragma unroll 2
-      for (int64_t t = kp * 32 + lane; t < k8; t += ks * 32) {
-        uint4 wv[NR];
+      // U of the weights' loads under way at once (past the row's end: zeros)
+      constexpr int U = NR == 1 ? 4 : 2;
+      for (int64_t t0 = kp * 32 + lane; t0 < k8; t0 += (int64_t)U * ks * 32) {
+        uint4 wv[U][NR];
 #pragma unroll
-        for (int c = 0; c < NR; ++c) wv[c] = __ldg(reinterpret_cast<const uint4 *>(wr[c]) + t);
-        uint4 xv[MR];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int r = 0; r < MR; ++r) xv[r] = __ldg(reinterpret_cast<const uint4 *>(xr[r]) + t);
+          for (int c = 0; c < NR; ++c)
+            wv[u][c] = load_if128(reinterpret_cast<const uint4 *>(wr[c]) + t0 + u * ks * 32, t0 + u * ks * 32 < k8);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          float xf[MR], wf[NR];
-#pragma unroll
-          for (int r = 0; r < MR; ++r) xf[r] = to_f32(reinterpret_cast<const T *>(&xv[r])[q]);
-#pragma unroll
-          for (int c = 0; c < NR; ++c) wf[c] = to_f32(reinterpret_cast<const T *>(&wv[c])[q]);
+        for (int u = 0; u < U; ++u) {
+          uint4 xv[MR];
 #pragma unroll
           for (int r = 0; r < MR; ++r)
+            xv[r] = load_if128(reinterpret_cast<const uint4 *>(xr[r]) + t0 + u * ks * 32, t0 + u * ks * 32 < k8);
 #pragma unroll
-            for (int c = 0; c < NR; ++c) acc[r][c] = fmaf(xf[r], wf[c], acc[r][c]);
+          for (int q = 0; q < 4; ++q) {
+            float2 xf[MR], wf[NR];
+#pragma unroll
+            for (int r = 0; r < MR; ++r) xf[r] = unpack2(reinterpret_cast<const uint32_t *>(&xv[r])[q], TypeCode<T>::code);
+#pragma unroll
+            for (int c = 0; c < NR; ++c) wf[c] = unpack2(reinterpret_cast<const uint32_t *>(&wv[u][c])[q], TypeCode<T>::code);
+#pragma unroll
+            for (int r = 0; r < MR; ++r)
+#pragma unroll
+              for (int c = 0; c < NR; ++c) acc2[r][c] = fma2(xf[r], wf[c], acc2[r][c]);
+          }
         }
       }
+#pragma unroll
+      for (int r = 0; r < MR; ++r)
+#pragma unroll
+        for (int c = 0; c < NR; ++c) acc[r][c] = acc2[r][c].x + acc2[r][c].y;
     }
     for (int64_t t = (vec ? k / 8 * 8 : 0) + kp * 32 + lane; t < k; t += ks * 32) {
       float wf[NR];
@@ -672,35 +685,37 @@ struct Saved {
 // dz = dy act'(z) rounded to T (unless dz is null), and the column sums of the
 // unrounded values over a block's rows -> sums[blockIdx.y] (unless null). Bound
 // by memory: dy and z read, dz written. A block's threads: x over columns, eight
-// each, y over rows; a thread takes four rows at a time, all loads first.
-// VEC: n is a multiple of 8 and dy and z take 16-byte accesses.
+// each, y over rows; a thread takes four rows at a time (two at other addresses,
+// which take twice the registers), all loads first. VEC: n is a multiple of 8 and dy
+// and z take 16-byte accesses.
 constexpr int kDzRows = 4;
 template <bool VEC, typename D, typename T>
 __global__ void __launch_bounds__(256, 3)
     dz_kernel(const D *dy, int64_t dy_ld, const Saved z, int act, int64_t m, int n, int rows_per_block, T *dz,
               int64_t dz_ld, float *sums) {
+  constexpr int R = VEC ? kDzRows : kDzRows / 2;
   __shared__ float part[256 * 8];
   const int j = (blockIdx.x * blockDim.x + threadIdx.x) * 8, count = max(0, min(8, n - j));
   const int64_t i1 = min(m, ((int64_t)blockIdx.y + 1) * rows_per_block);
   float2 acc[4] = {};
   const int step = blockDim.y;
   grid_launch();
-  for (int64_t i0 = (int64_t)blockIdx.y * rows_per_block + threadIdx.y; i0 < i1 && count > 0; i0 += kDzRows * step) {
-    Eight<D> v[kDzRows];
-    Eight<T> s[kDzRows];
-    float down[kDzRows];
+  for (int64_t i0 = (int64_t)blockIdx.y * rows_per_block + threadIdx.y; i0 < i1 && count > 0; i0 += R * step) {
+    Eight<D> v[R];
+    Eight<T> s[R];
+    float down[R];
     const int there = VEC ? 8 : count;
     const void *dy_end = dy + (m - 1) * dy_ld + n, *z_end = static_cast<const T *>(z.p) + (m - 1) * z.ld + n;
 #pragma unroll
-    for (int u = 0; u < kDzRows; ++u) v[u] = fetch_eight<D>(dy + min(i0 + u * step, i1 - 1) * dy_ld + j, VEC, there, dy, dy_end);
+    for (int u = 0; u < R; ++u) v[u] = fetch_eight<D>(dy + min(i0 + u * step, i1 - 1) * dy_ld + j, VEC, there, dy, dy_end);
     if (act != NR_ACT_NONE) {
       if (!z.scale) {
 #pragma unroll
-        for (int u = 0; u < kDzRows; ++u)
+        for (int u = 0; u < R; ++u)
           s[u] = fetch_eight<T>(static_cast<const T *>(z.p) + min(i0 + u * step, i1 - 1) * z.ld + j, VEC, there, z.p, z_end);
       } else {
 #pragma unroll
-        for (int u = 0; u < kDzRows; ++u) {
+        for (int u = 0; u < R; ++u) {
           const int64_t i = min(i0 + u * step, i1 - 1);
           const uint2 c = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(z.p) + i * z.groups * kOpsGroup + j));
           s[u].r[0] = c.x, s[u].r[1] = c.y;
@@ -709,7 +724,7 @@ __global__ void __launch_bounds__(256, 3)
       }
     }
 #pragma unroll
-    for (int u = 0; u < kDzRows; ++u) {
+    for (int u = 0; u < R; ++u) {
       const int64_t i = i0 + u * step;
       if (i >= i1) break;
       settle_eight<D>(v[u], dy + i * dy_ld + j, VEC, there, dy, dy_end);
@@ -729,8 +744,17 @@ __global__ void __launch_bounds__(256, 3)
 #pragma unroll
           for (int q = 0; q < 4; ++q) p[q] = pair_of<T>(s[u], q);
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) d[q] = mul2(d[q], act_slope2(p[q], act));
+        // one test of the activation for the eight
+#define NR_SLOPE(A)                   \
+  _Pragma("unroll") for (int q = 0; q < 4; ++q) d[q] = mul2(d[q], act_slope2(p[q], A));
+        if (act == NR_ACT_GELU) {
+          NR_SLOPE(NR_ACT_GELU)
+        } else if (act == NR_ACT_SILU) {
+          NR_SLOPE(NR_ACT_SILU)
+        } else {
+          NR_SLOPE(NR_ACT_RELU)
+        }
+#undef NR_SLOPE
       }
       // the pitch is a multiple of 8
       if (dz) *reinterpret_cast<uint4 *>(dz + i * dz_ld + j) = pack8(d, TypeCode<T>::code);
@@ -937,7 +961,7 @@ nr_status products(const Task *t, int count, Finish &F, int device, bool follows
                 : launch_product<2>(maps, J, smem, grid, device, follows, s);
     follows = true;
   }
-  const int64_t blocks = (int64_t)F.blocks[0] + F.blocks[1] + (F.dbias ? ceil_div(F.sums_n, 32) : 0);
+  const int64_t blocks = (int64_t)F.blocks[0] + F.blocks[1] + (F.dbias ? ceil_div(F.sums_n, 8) : 0);
   if (e == cudaSuccess && blocks > 0) e = launch(finish_kernel, (unsigned)blocks, dim3(256), 0, s, follows, F);
   return e == cudaSuccess ? NR_OK : cuda_status(e);
 }
@@ -1042,7 +1066,7 @@ void launch_rows_any(const nr_linear *a, const Epilogue &E, int sms, cudaStream_
 }
 
 // dz_kernel's blocks: threads across up to 256 columns, rows of few columns share a
-// block; enough blocks for the GPU, at most 256 rows of column sums to add
+// block; enough blocks for the GPU, at most 1024 rows of column sums to add
 struct DzCut {
   dim3 block;
   int gx, gy, rows;
@@ -1055,7 +1079,7 @@ DzCut cut_dz(int64_t m, int64_t n, int sms) {
   c.gx = (int)ceil_div(n, (int64_t)bx * 8);
   const int64_t most = ceil_div((int64_t)sms * 6, c.gx);
   const int64_t step = kDzRows * (int64_t)c.block.y;
-  c.rows = (int)round_up(ceil_div(m, most < 256 ? most : 256), step);
+  c.rows = (int)round_up(ceil_div(m, most < 1024 ? most : 1024), step);
   c.gy = (int)ceil_div(m, c.rows);
   return c;
 }

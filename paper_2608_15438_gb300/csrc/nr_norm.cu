@@ -52,8 +52,7 @@ struct Norm {
   const void *x_end, *dy_end, *dres_end;  // past the matrices' last values
   float *parts;  // [blocks][2][n]: the blocks' sums for dweight, dbias
   int eights;    // a thread's columns come in eights
-  int vec;       // and every matrix takes 16-byte accesses
-  int w_vec;     // as do weight and bias
+  int vec;       // and every matrix, weight and bias take 16-byte accesses
 };
 
 // the column of element q of the thread's v-th eight, of a group of TPR threads
@@ -72,6 +71,14 @@ __device__ __forceinline__ uint32_t load_if32(const void *p, bool in) {
       : "l"(p), "r"((int)in));
   return v;
 }
+__device__ __forceinline__ uint16_t load_if16(const void *p, bool in) {
+  uint16_t v;
+  asm("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n mov.b16 %0, 0;\n @p ld.global.nc.b16 %0, [%1];\n}\n"
+      : "=h"(v)
+      : "l"(p), "r"((int)in));
+  return v;
+}
+
 template <int TPR, typename T>
 __device__ __forceinline__ Eight<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, const void *lo, const void *hi,
                                              int width = TPR) {
@@ -146,13 +153,20 @@ __device__ __forceinline__ void load_w(const void *p, int dtype, float none, int
                                        float2 (&w)[4], int width = TPR) {
   float o[8];
   const int c = column<TPR>(eights, v, 0, t, width);
-  if (p && vec) {
+  const int st = eights ? 1 : TPR ? TPR : width;
+  if (!p) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = none;
+  } else if (vec) {  // known when compiled
     load8(p, c < n ? c : 0, dtype, 1, 8, o);
+  } else if (dtype == NR_F32) {  // one test of the type, all loads under way at once
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = __uint_as_float(load_if32(static_cast<const float *>(p) + c + q * st, c + q * st < n));
   } else {
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const int cq = eights ? c + q : c + q * (TPR ? TPR : width);
-      o[q] = p && cq < n ? load_any(p, cq, dtype) : none;
+      const uint32_t h = load_if16(static_cast<const uint16_t *>(p) + c + q * st, c + q * st < n);
+      o[q] = unpack2(h, dtype).x;
     }
   }
 #pragma unroll
@@ -425,11 +439,10 @@ template <int TPR, int V, bool VEC, typename T>
 __global__ void __launch_bounds__(kWarpThreads, V == 6 ? 5 : 4) warp_forward_kernel(const Norm N) {
   constexpr int R = V == 6 ? 1 : V == 3 ? 2 : 4, kGroups = kWarpThreads / TPR;
   const int t = threadIdx.x % TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
-  const bool w_vec = VEC && N.w_vec;
   float2 w[4], b[4];  // V = 1: a thread's own, kept
   if (V == 1) {
-    load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, w_vec, 0, t, n, w);
-    load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, w_vec, 0, t, n, b);
+    load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, 0, t, n, w);
+    load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, VEC, 0, t, n, b);
   }
   // a block's groups take the same number of turns, so that shuffles are complete
   for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
@@ -440,8 +453,8 @@ __global__ void __launch_bounds__(kWarpThreads, V == 6 ? 5 : 4) warp_forward_ker
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (V > 1) {
-        load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w);
-        load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, w_vec, v, t, n, b);
+        load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w);
+        load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, VEC, v, t, n, b);
       }
       F.write(N, i, v, t, eights, TPR, w, b);
     }
@@ -456,7 +469,7 @@ __global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const No
   __shared__ float sums[2][TPR * 8];
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
   float2 w[4], dw[4] = {}, db[4] = {};
-  load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC && N.w_vec, 0, t, n, w);
+  load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, 0, t, n, w);
   for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
     const int64_t i = i0 + group * R;
     Backward<TPR, 1, R, VEC, T> G;
@@ -496,7 +509,6 @@ template <int V, int R, int THREADS, bool VEC, typename T>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) block_forward_kernel(const Norm N) {
   __shared__ BlockSums<R> S;
   const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
-  const bool w_vec = VEC && N.w_vec;
   int turn = 0;
   for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
     Forward<0, V, R, VEC, T> F;
@@ -504,8 +516,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float2 w[4], b[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
-      load_w<0>(N.bias, N.w_dtype, 0.0f, eights, w_vec, v, t, n, b, width);
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
+      load_w<0>(N.bias, N.w_dtype, 0.0f, eights, VEC, v, t, n, b, width);
       F.write(N, i, v, t, eights, width, w, b);
     }
     if (N.mean && t == 0) F.write_statistics(N, i);
@@ -520,7 +532,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ?
   extern __shared__ float sums[];  // [2][n], with several groups
   const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
   const int group = THREADS == 384 ? threadIdx.y : 0, groups = THREADS == 384 ? blockDim.y : 1;
-  const bool w_vec = VEC && N.w_vec;
   float2 dw[V][4] = {}, db[V][4] = {};
   int turn = 0;
   for (int64_t i = ((int64_t)blockIdx.x * groups + group) * R; i < N.m; i += (int64_t)gridDim.x * groups * R) {
@@ -529,7 +540,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ?
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float2 w[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
       G.add(v, w, dw[v], db[v]);
     }
     block_sums<2 * R>(G.s, S, turn++, t, width, group);
@@ -537,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ?
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float2 w[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, w_vec, v, t, n, w, width);
+      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
       G.write(N, i, v, t, eights, width, w);
     }
   }
@@ -699,13 +710,13 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
           (!a->residual_grad || vec_ok(a->residual_grad, a->residual_grad_ld, dt));
   else
     vec = vec && vec_ok(a->y, a->y_ld, dt);
+  vec = vec && vec_ok(a->weight, 8, a->w_dtype) && vec_ok(a->bias, 8, a->w_dtype);
   N.vec = vec;
   N.eights = vec || a->x_scale || dt != NR_F32;
   const int64_t e = (int64_t)type_bytes(dt);
   N.x_end = static_cast<const char *>(a->x) + ((a->m - 1) * a->x_ld + a->n) * e;
   N.dy_end = static_cast<const char *>(a->dy) + ((a->m - 1) * a->dy_ld + a->n) * e;
   N.dres_end = static_cast<const char *>(a->residual_grad) + ((a->m - 1) * a->residual_grad_ld + a->n) * e;
-  N.w_vec = N.eights && a->n % 8 == 0 && vec_ok(a->weight, 8, a->w_dtype) && vec_ok(a->bias, 8, a->w_dtype);
   return N;
 }
 
