@@ -6,7 +6,10 @@ Argument checks and marshalling only; every step runs in the library's
 kernels and there is no fallback. Matrices are CUDA tensors of two dimensions
 with any row pitch (stride(1) == 1); a wrong tensor raises before any call.
 Work goes to the current stream of the tensors' device, or to `stream`, on
-which the outputs are then allocated. Nothing synchronises.
+which the outputs are then allocated (the caller orders the streams, as for any
+tensor used on another than its own). Nothing synchronises, and a CUDA graph may
+capture the calls. The outputs carry no autograd history; residual.py wraps the
+calls in autograd functions.
 """
 from __future__ import annotations
 
@@ -30,7 +33,18 @@ class Checkpoint8:
     __slots__ = ("codes", "scales", "shape", "dtype")
 
     def __init__(self, codes, scales, shape, dtype):
-        self.codes, self.scales, self.shape, self.dtype = codes, scales, tuple(shape), dtype
+        m, n = (int(v) for v in shape)
+        g = -(-n // _GROUP)
+        if dtype not in _DT:
+            raise ValueError(f"dtype: {dtype}, expected {' or '.join(map(str, _DT))}")
+        for t, name, dt, cols in ((codes, "codes", torch.int8, g * _GROUP), (scales, "scales", torch.uint8, g)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+            if t.dtype != dt or t.shape != (m, cols) or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"{name}: expected a contiguous CUDA tensor {dt} of shape {(m, cols)}")
+        if codes.device != scales.device or codes.data_ptr() % 16:
+            raise ValueError("codes and scales: on one device, codes 16-byte aligned")
+        self.codes, self.scales, self.shape, self.dtype = codes, scales, (m, n), dtype
 
     @property
     def device(self):
@@ -140,8 +154,11 @@ def _scratch(call, nbytes, device):
 
 def _new_checkpoint(m, n, dtype, device):
     g = -(-n // _GROUP)
-    return Checkpoint8(torch.empty((m, g * _GROUP), dtype=torch.int8, device=device),
-                       torch.empty((m, g), dtype=torch.uint8, device=device), (m, n), dtype)
+    c = Checkpoint8.__new__(Checkpoint8)
+    c.codes = torch.empty((m, g * _GROUP), dtype=torch.int8, device=device)
+    c.scales = torch.empty((m, g), dtype=torch.uint8, device=device)
+    c.shape, c.dtype = (m, n), dtype
+    return c
 
 
 def checkpoint8(x, stream=None) -> Checkpoint8:

@@ -501,6 +501,10 @@ def test_refusals(ops):
         (ValueError, "residual_grad", lambda: ops.layer_norm_backward(x, x, None, b[:8], b[:8], residual_grad=x.float())),
         (ValueError, "dtype", lambda: ops.checkpoint8(x.to(torch.int8))),
         (TypeError, "Checkpoint8", lambda: ops.checkpoint8_read(x)),
+        (ValueError, "codes", lambda: ops.Checkpoint8(torch.zeros(8, 16, device="cuda", dtype=torch.int8),
+                                                      torch.zeros(8, 1, device="cuda", dtype=torch.uint8), (8, 16), BF16)),
+        (ValueError, "scales", lambda: ops.Checkpoint8(torch.zeros(8, 32, device="cuda", dtype=torch.int8),
+                                                       torch.zeros(8, 2, device="cuda", dtype=torch.uint8), (8, 16), BF16)),
     ]
     for kind, text, call in bad:
         with pytest.raises(kind, match=text):
