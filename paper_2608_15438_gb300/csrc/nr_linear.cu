@@ -82,34 +82,53 @@ __device__ __forceinline__ void add_raw(float2 (&v)[4], const uint4 &r, int dtyp
   v[0] = add2(v[0], unpack2(r.x, dtype)), v[1] = add2(v[1], unpack2(r.y, dtype));
   v[2] = add2(v[2], unpack2(r.z, dtype)), v[3] = add2(v[3], unpack2(r.w, dtype));
 }
+// eight 16-bit values of a row, of which `count` are there, the four threads of 32
+// columns together (lanes 4 a .. 4 a + 3 of a warp); vec: at 16-byte addresses
+__device__ __forceinline__ void store_any16(uint16_t *p, int vec, int count, const float2 (&v)[4], int dtype) {
+  const int lane = threadIdx.x & 31;
+  const uint4 o = pack8(v, dtype);
+  if (vec && count == 8) {
+    *reinterpret_cast<uint4 *>(p) = o;
+    return;
+  }
+  const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+  if (vec) {  // a row's end, which is this lane's alone
+#pragma unroll
+    for (int q = 0; q < 7; ++q)
+      if (q < count) p[q] = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
+    return;
+  }
+  store16x8(p, count, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
+}
+
 // Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'), row_ok
 // false for rows past the end; called as hold8 is.
 __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, bool row_ok, float2 (&v)[4],
                                         const float2 (&bias)[4]) {
-  const int count = row_ok ? min(8, (int)E.n - j) : 0;  // may be negative
+  const int count = row_ok ? max(0, min(8, (int)E.n - j)) : 0;
+  const uint16_t *pr = static_cast<const uint16_t *>(E.residual) + i * E.residual_ld + j;
+  uint32_t res[8];
+  if (E.residual) fetch16x8(pr, count, E.residual, E.residual_end, res);
 #pragma unroll
   for (int q = 0; q < 4; ++q) v[q] = add2(v[q], bias[q]);
   if (E.z) {
-    if (E.z_scale) {
-      hold8(E, i, j, row_ok, count, v);
-    } else if (count > 0) {
-      const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
-      store8(E.z, i * E.z_ld + j, E.dtype, E.z_vec, count, o);
-    }
+    if (E.z_scale) hold8(E, i, j, row_ok, count, v);
+    else store_any16(static_cast<uint16_t *>(E.z) + i * E.z_ld + j, E.z_vec, count, v, E.dtype);
   }
-  if (count <= 0) return;
   if (E.act != NR_ACT_NONE) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = act_value2(v[q], E.act);
   }
   if (E.residual) {
-    float r[8];
-    load8(E.residual, i * E.residual_ld + j, E.dtype, E.residual_vec, count, r);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = add2(v[q], make_float2(r[2 * q], r[2 * q + 1]));
+    settle16x8(pr, count, E.residual, E.residual_end, res);
+    add_raw(v, make_uint4(res[0], res[1], res[2], res[3]), E.dtype);
   }
-  const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
-  store8(E.y, i * E.y_ld + j, E.y_dtype, E.y_vec, count, o);
+  if (E.y_dtype == NR_F32) {
+    const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
+    if (count > 0) store8(E.y, i * E.y_ld + j, NR_F32, E.y_vec, count, o);
+  } else {
+    store_any16(static_cast<uint16_t *>(E.y) + i * E.y_ld + j, E.y_vec, count, v, E.dtype);
+  }
 }
 
 __device__ __forceinline__ void bias8(const Epilogue &E, int j, float2 (&b)[4]) {
@@ -147,28 +166,29 @@ __device__ __forceinline__ void stage_read(const float *stage, int lane, int u, 
 
 // eight 16-bit values of a row: the four threads of 32 columns together
 template <bool VEC>
-__device__ __forceinline__ void store_block(uint16_t *p, int lane, const float2 (&v)[4], int dtype) {
+__device__ __forceinline__ void store_block(uint16_t *p, bool there, int lane, const float2 (&v)[4], int dtype) {
   const uint4 o = pack8(v, dtype);
   if (VEC) {
-    *reinterpret_cast<uint4 *>(p) = o;
+    if (there) *reinterpret_cast<uint4 *>(p) = o;
   } else {
     const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-    store16x8(p, 8, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
+    store16x8(p, there ? 8 : 0, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
   }
 }
 
-// A whole block (32 rows and columns there, y 16-bit) from row i, column j of the
-// thread's eight: no bounds, one test a step for all rows. VEC: every matrix takes
+// A block with its 32 columns there and y 16-bit, from row i, column j of the
+// thread's eight of four rows, of which those below `left` rows on are there: one
+// test a step for all rows. VEC: every matrix takes
 // 16-byte accesses, and res holds the residual, loaded ahead.
 template <bool VEC>
-__device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j, const float *stage, int lane,
+__device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int left, int j, const float *stage, int lane,
                                              const float2 (&b)[4], const uint4 (&res)[4]) {
   float2 v[4][4];
   uint32_t far[4][8];
   const uint16_t *pr = static_cast<const uint16_t *>(E.residual) + i * E.residual_ld + j;
   if (!VEC && E.residual) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) fetch16x8(pr + 8 * u * E.residual_ld, 8, E.residual, E.residual_end, far[u]);
+    for (int u = 0; u < 4; ++u) fetch16x8(pr + 8 * u * E.residual_ld, 8 * u < left ? 8 : 0, E.residual, E.residual_end, far[u]);
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -179,11 +199,11 @@ __device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j
   if (E.z) {
     if (E.z_scale) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) hold8(E, i + 8 * u, j, true, 8, v[u]);
+      for (int u = 0; u < 4; ++u) hold8(E, i + 8 * u, j, 8 * u < left, 8, v[u]);
     } else {
       uint16_t *z = static_cast<uint16_t *>(E.z) + i * E.z_ld + j;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) store_block<VEC>(z + 8 * u * E.z_ld, lane, v[u], E.dtype);
+      for (int u = 0; u < 4; ++u) store_block<VEC>(z + 8 * u * E.z_ld, 8 * u < left, lane, v[u], E.dtype);
     }
   }
 #define NR_BLOCK_ACT(A)                                  \
@@ -203,14 +223,14 @@ __device__ __forceinline__ void finish_block(const Epilogue &E, int64_t i, int j
       if (VEC) {
         add_raw(v[u], res[u], E.dtype);
       } else {
-        settle16x8(pr + 8 * u * E.residual_ld, 8, E.residual, E.residual_end, far[u]);
+        settle16x8(pr + 8 * u * E.residual_ld, 8 * u < left ? 8 : 0, E.residual, E.residual_end, far[u]);
         add_raw(v[u], make_uint4(far[u][0], far[u][1], far[u][2], far[u][3]), E.dtype);
       }
     }
   }
   uint16_t *y = static_cast<uint16_t *>(E.y) + i * E.y_ld + j;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) store_block<VEC>(y + 8 * u * E.y_ld, lane, v[u], E.dtype);
+  for (int u = 0; u < 4; ++u) store_block<VEC>(y + 8 * u * E.y_ld, 8 * u < left, lane, v[u], E.dtype);
 }
 
 // ------------------------------------------------------------ products on tensor cores
@@ -448,11 +468,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       item_of(P, second ? item - J.items0 : item, tm, tn, part);
       const uint32_t a = it & 1u;
       const int64_t i0 = ((int64_t)tm * CG + rank) * kRows + lg * 32;
-      const bool blocks = E.y_dtype != NR_F32 && !partial && i0 + 32 <= rows;
+      const bool blocks = E.y_dtype != NR_F32 && !partial;
+      const int left = (int)min(rows - i0, (int64_t)32) - r8;  // rows from the thread's first on
       const bool vectors = E.y_vec && (!E.z || E.z_scale || E.z_vec) && (!E.residual || E.residual_vec);
       // the two warps of a lane quarter take its chunks of 32 columns in turn
       const int c0 = tn * P.nt + (ew >> 2) * 32, c1 = i0 < rows ? min(n, (tn + 1) * P.nt) : 0;
-      if (E.residual && blocks) {  // the residual's way from memory, while the sums are made
+      if (E.residual && blocks && i0 + lane < rows) {  // the residual's way from memory, while the sums are made
         const uint16_t *p = static_cast<const uint16_t *>(E.residual) + (i0 + lane) * E.residual_ld;
         for (int c = c0; c < c1; c += 64) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p + c));
       }
@@ -477,16 +498,16 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         if (E.residual && whole && vectors) {
           const uint16_t *p = static_cast<const uint16_t *>(E.residual) + (i0 + r8) * E.residual_ld + j;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) res[u] = __ldg(reinterpret_cast<const uint4 *>(p + 8 * u * E.residual_ld));
+          for (int u = 0; u < 4; ++u) res[u] = load_if128(p + 8 * u * E.residual_ld, 8 * u < left);
         }
         tc::wait_ld(v);
         __syncwarp();  // the block's previous readers are done
         stage_write(stage, lane, v);
         __syncwarp();
         if (whole && vectors) {
-          finish_block<true>(E, i0 + r8, j, stage, lane, b, res);
+          finish_block<true>(E, i0 + r8, left, j, stage, lane, b, res);
         } else if (whole) {
-          finish_block<false>(E, i0 + r8, j, stage, lane, b, res);
+          finish_block<false>(E, i0 + r8, left, j, stage, lane, b, res);
         } else {
 #pragma unroll 1
           for (int u = 0; u < 4; ++u) {
@@ -912,8 +933,15 @@ cudaError_t launch_product(const CUtensorMap (&m)[4], const Job &J, uint32_t sme
 // The products of one or two tasks (of the same CTAs a tile) in one launch, and
 // what is left to finish, with the column sums' last addition, in another.
 // follows: the call has launched before.
-nr_status products(const Task *t, int count, Finish &F, int device, bool follows, cudaStream_t s) {
+nr_status products(Task *t, int count, Finish &F, int device, bool follows, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
+  // the longer items first: the last turn is then a short one (36696 x 496 -> 170
+  // backward 87 -> 74 us)
+  if (count == 2 && ceil_div(t[1].inner, t[1].c.splits) * t[1].c.nt > ceil_div(t[0].inner, t[0].c.splits) * t[0].c.nt) {
+    const Task first = t[1];
+    t[1] = t[0];
+    t[0] = first;
+  }
   Job J = {};
   if (count > 0) {
     e = nr_ops_flag(device, &J.flag);
@@ -1047,8 +1075,11 @@ void launch_rows(const nr_linear *a, const Epilogue &E, int sms, cudaStream_t s)
   const T *x = static_cast<const T *>(a->x), *w = static_cast<const T *>(a->w);
   const int vec = vec_ok(a->x, a->x_ld, a->dtype) && vec_ok(a->w, a->w_ld, a->dtype);
   const int64_t want = sms * kRowsWarps;
-  // four columns a warp where that fills the GPU, else one and t split over warps
-  const int nr = a->n >= 4 * want ? 4 : 1;
+  // Four columns a warp where that fills the GPU, with t in parts for four rows and
+  // more, whose conversions for one column cost more than its products (1536 ->
+  // 6144: four rows 11.0 -> 8.4 us, eight 18.2 -> 15.6). Else one column, and t split
+  // over warps.
+  const int nr = a->n >= 4 * want || (MR >= 4 && a->n * (a->k / 512) >= 4 * want && a->n >= want) ? 4 : 1;
   int ks = 1;
   while (ks < kRowsThreads / 32 && ceil_div(a->n, nr) * ks < want && a->k / (ks * 2) >= 256) ks *= 2;
   const unsigned blocks = (unsigned)ceil_div(ceil_div(a->n, nr), kRowsThreads / 32 / ks);
@@ -1203,7 +1234,7 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
     if (f.w_at >= 0) f.w = o[packs - 1];
   }
   Finish F = {};
-  const Task t = {f.x, f.w, a->m, a->k, f.cut, E, static_cast<float *>(at(ws, f.parts_at))};
+  Task t = {f.x, f.w, a->m, a->k, f.cut, E, static_cast<float *>(at(ws, f.parts_at))};
   return products(&t, 1, F, device, packs > 0, s);
 }
 
