@@ -159,6 +159,8 @@ __device__ __forceinline__ void load_w(const void *p, int dtype, float none, int
     for (int q = 0; q < 8; ++q) o[q] = none;
   } else if (vec) {  // known when compiled
     load8(p, c < n ? c : 0, dtype, 1, 8, o);
+  } else if (eights && c + 8 <= n && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {  // rows end anywhere, the weights begin well
+    load8(p, c, dtype, 1, 8, o);
   } else if (dtype == NR_F32) {  // one test of the type, all loads under way at once
 #pragma unroll
     for (int q = 0; q < 8; ++q) o[q] = __uint_as_float(load_if32(static_cast<const float *>(p) + c + q * st, c + q * st < n));
@@ -235,21 +237,32 @@ __device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int t
 // m on are skipped (they hold zeros).
 template <int TPR, int V, int R, bool VEC, typename T>
 struct Forward {
+  // Rows of 16 bits are loaded a turn ahead, so that loads are under way during the
+  // sums (2^20 x 128: 105 -> 86 us, 65536 x 4096: 330 -> 280 us; backward, where a
+  // row's registers are twice as many, half the rows a turn and the next ones
+  // ahead took 573 us for 450 at 262144 x 1536).
+  static constexpr bool kAhead = VEC && sizeof(T) == 2;
+  Eight<T> raw[R][V];
   float2 x[R][V][4];
   float mean[R], rstd[R];
 
+  __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int width) {
+    const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, (int)N.n, N.x.p, N.x_end, width)
+                                : Eight<T>{};
+  }
+  // rows i on, `next` the turn after's
   template <typename Sums>
-  __device__ __forceinline__ void statistics(const Norm &N, int64_t i, int t, int eights, int width, Sums sums) {
+  __device__ __forceinline__ void statistics(const Norm &N, int64_t i, int64_t next, int t, int eights, int width, Sums sums) {
     const int n = (int)N.n;
     const float inv = 1.0f / (float)n;
-    Eight<T> raw[R][V];
     if (!N.x.scale) {
       const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, n, N.x.p, N.x_end, width) : Eight<T>{};
+      if (!kAhead) load(N, i, t, eights, width);
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -258,6 +271,7 @@ struct Forward {
 #pragma unroll
           for (int q = 0; q < 4; ++q) x[r][v][q] = pair_of<T>(raw[r][v], q);
         }
+      if (kAhead) load(N, next, t, eights, width);
     } else {
       float scale[R][V];
 #pragma unroll
@@ -341,6 +355,18 @@ struct Backward {
   __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int width) {
     const int n = (int)N.n;
     const T *pd = static_cast<const T *>(N.dy) + i * N.dy_ld, *px = static_cast<const T *>(N.x.p) + i * N.x.ld;
+    // the residual's gradient into L2 while the sums are made, a line for the eight
+    // threads that read it (65536 x 1536 in bf16: 180 -> 162 us; fp32 gained nothing)
+    if (VEC && sizeof(T) == 2 && N.dres && (t & 7) == 0) {
+      const T *pr = static_cast<const T *>(N.dres) + i * N.dres_ld;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int c = column<TPR>(1, v, 0, t, width);
+          if (i + r < N.m && c < n) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(pr + r * N.dres_ld + c));
+        }
+    }
     // one branch around all loads, so that they are under way together; rows past
     // the end hold zeros and add nothing
 #pragma unroll
@@ -436,7 +462,7 @@ struct Backward {
 constexpr int kWarpThreads = 128;
 
 template <int TPR, int V, bool VEC, typename T>
-__global__ void __launch_bounds__(kWarpThreads, V == 6 ? 5 : 4) warp_forward_kernel(const Norm N) {
+__global__ void __launch_bounds__(kWarpThreads, 4) warp_forward_kernel(const Norm N) {
   constexpr int R = V == 6 ? 1 : V == 3 ? 2 : 4, kGroups = kWarpThreads / TPR;
   const int t = threadIdx.x % TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
   float2 w[4], b[4];  // V = 1: a thread's own, kept
@@ -444,11 +470,13 @@ __global__ void __launch_bounds__(kWarpThreads, V == 6 ? 5 : 4) warp_forward_ker
     load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, 0, t, n, w);
     load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, VEC, 0, t, n, b);
   }
+  const int64_t stride = (int64_t)gridDim.x * kGroups * R;
+  Forward<TPR, V, R, VEC, T> F;
+  if (F.kAhead && !N.x.scale) F.load(N, (int64_t)blockIdx.x * kGroups * R + threadIdx.x / TPR * R, t, eights, TPR);
   // a block's groups take the same number of turns, so that shuffles are complete
-  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
+  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += stride) {
     const int64_t i = i0 + threadIdx.x / TPR * R;
-    Forward<TPR, V, R, VEC, T> F;
-    F.statistics(N, i, t, eights, TPR, [](float(&v)[R]) { lane_sums<TPR, R>(v); });
+    F.statistics(N, i, i + stride, t, eights, TPR, [](float(&v)[R]) { lane_sums<TPR, R>(v); });
     if (V > 1) forget();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -510,9 +538,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) 
   __shared__ BlockSums<R> S;
   const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
   int turn = 0;
-  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += (int64_t)gridDim.x * R) {
-    Forward<0, V, R, VEC, T> F;
-    F.statistics(N, i, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++, t, width, 0); });
+  const int64_t stride = (int64_t)gridDim.x * R;
+  Forward<0, V, R, VEC, T> F;
+  if (F.kAhead && !N.x.scale) F.load(N, (int64_t)blockIdx.x * R, t, eights, width);
+  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += stride) {
+    F.statistics(N, i, i + stride, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++, t, width, 0); });
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float2 w[4], b[4];
@@ -729,12 +759,16 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
 struct Shape {
   int tpr, v, threads, groups;  // threads a row's group, groups a block
 };
-Shape shape_of(int64_t n, bool vec, bool backward) {
+Shape shape_of(int64_t n, bool vec, bool small, bool backward) {
   if (n <= 256) return {n <= 64 ? 8 : n <= 128 ? 16 : 32, 1, kWarpThreads, 1};
   if (!backward && vec && n <= 768) return {32, 3, kWarpThreads, 1};
   if (!backward && vec && n <= 1536) return {32, 6, kWarpThreads, 1};
   if (n > kLong) return {0, 0, 0, 0};
-  const int v = n > 8192 ? 4 : n > (backward ? 2048 : 4096) ? 2 : 1;
+  // forward with aligned rows: as many eights as leave a block 256 threads, since
+  // the rows of three such blocks an SM wait less for each other at the sums'
+  // barriers than two of 512 (65536 x 4096: 212 us, 280 by 512 threads)
+  const bool wide = backward ? n > 2048 : n > (vec ? 2048 : 4096);
+  const int v = n > (vec && small && !backward ? 4096 : 8192) ? 4 : wide ? 2 : 1;
   const int threads = (int)round_up(ceil_div(n, 8 * v), 32);
   // groups side by side up to 384 threads: rows of 387 in fp32 leave 304 blocks'
   // sums instead of 1824 to add (23 us); rows of 1536 ran 15% slower so
@@ -747,12 +781,13 @@ Shape shape_of(int64_t n, bool vec, bool backward) {
 int block_count(const Shape &s, int64_t m, bool backward, bool vec, int sms) {
   int per_sm, rows = s.groups;
   if (s.tpr) {
-    per_sm = s.v == 6 ? 5 : 4;
+    per_sm = 4;
     rows = kWarpThreads / s.tpr;
   } else if (backward && s.v == 1) {
     per_sm = 768 / (s.threads * s.groups);
   } else {
-    per_sm = (!backward && s.v < 4 ? s.threads <= 256 ? 768 : 1024 : backward && s.v == 2 && !vec ? 580 : 512) / s.threads;
+    const int held = !backward ? s.threads <= 256 ? 768 : s.v < 4 ? 1024 : 512 : s.v == 2 && !vec ? 580 : 512;
+    per_sm = held / s.threads;
   }
   const int64_t need = ceil_div(m, rows), most = (int64_t)sms * per_sm;
   return (int)(need < most ? need : most);
@@ -772,6 +807,8 @@ cudaError_t forward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_
   else if (s.tpr) warp_forward_kernel<32, 6, true, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1 && th <= 256) block_forward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1) block_forward_kernel<1, 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  else if (VEC && s.v == 2 && th <= 256) block_forward_kernel<2, sizeof(T) == 2 ? 2 : 1, 256, true, T><<<blocks, th, 0, st>>>(N);
+  else if (VEC && s.v == 4 && th <= 256) block_forward_kernel<4, 1, 256, true, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 2) block_forward_kernel<2, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
   else block_forward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
   return cudaGetLastError();
@@ -812,7 +849,7 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
   if (!g.ok) return NR_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Norm N = norm_of(a, false);
-  const Shape sh = shape_of(a->n, N.vec, false);
+  const Shape sh = shape_of(a->n, N.vec, a->dtype != NR_F32, false);
   cudaError_t e;
   if (sh.threads) {
     e = launch_any(N, sh, false, a->dtype, block_count(sh, a->m, false, N.vec, nr_ops_sms(device)), s);
@@ -827,7 +864,7 @@ extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int 
   if (!valid(a, true)) return -1;
   if (a->m == 0 || !a->dweight) return 0;
   const bool vec = norm_of(a, true).vec;
-  const Shape sh = shape_of(a->n, vec, true);
+  const Shape sh = shape_of(a->n, vec, a->dtype != NR_F32, true);
   const int64_t blocks = sh.threads ? block_count(sh, a->m, true, vec, nr_ops_sms(device)) : kLongParts;
   return round_up(blocks * 2 * a->n * 4, 256);
 }
@@ -849,7 +886,7 @@ extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, 
   }
   Norm N = norm_of(a, true);
   N.parts = a->dweight ? static_cast<float *>(ws) : nullptr;
-  const Shape sh = shape_of(a->n, N.vec, true);
+  const Shape sh = shape_of(a->n, N.vec, a->dtype != NR_F32, true);
   int parts = kLongParts;
   if (sh.threads) {
     parts = block_count(sh, a->m, true, N.vec, nr_ops_sms(device));
