@@ -26,6 +26,18 @@
 
 namespace {
 
+// How the matrices lie. kVec: every eight of a row's columns at a 16-byte address.
+// kPhase: the matrices' rows start at the same distance from 16-byte addresses, as
+// contiguous matrices of any width do. Rows a step (16 bytes' values) apart then start
+// alike, and a block takes only such rows: its threads hold the aligned sixteen bytes
+// of them as in kVec, from `lead` values before a row's first one on, and only a row's
+// ends need care (65536 x 1659 in fp16 against kAny: forward 163 us for 282, backward
+// 201 for 333; 65536 x 3001 in fp32: 337 for 503, 484 for 875).
+// kAny: everything else.
+enum Lie { kAny, kVec, kPhase };
+template <int A, typename T>
+constexpr int kStepOf = A == kPhase ? 16 / (int)sizeof(T) : 1;
+
 // values of a type, or a checkpoint's codes and scales
 struct Rows {
   const void *p;
@@ -52,7 +64,7 @@ struct Norm {
   const void *x_end, *dy_end, *dres_end;  // past the matrices' last values
   float *parts;  // [blocks][2][n]: the blocks' sums for dweight, dbias
   int eights;    // a thread's columns come in eights
-  int vec;       // and every matrix, weight and bias take 16-byte accesses
+  int lie;       // Lie
 };
 
 // the column of element q of the thread's v-th eight, of a group of TPR threads
@@ -79,11 +91,30 @@ __device__ __forceinline__ uint16_t load_if16(const void *p, bool in) {
   return v;
 }
 
-template <int TPR, typename T>
-__device__ __forceinline__ Eight<T> load_raw(const T *row, int eights, bool vec, int v, int t, int n, const void *lo, const void *hi,
+// (kPhase: row, weights and n count from `lead` values before the row)
+template <int TPR, int A, typename T>
+__device__ __forceinline__ Eight<T> load_raw(const T *row, int eights, int v, int t, int lead, int n, const void *lo, const void *hi,
                                              int width = TPR) {
   const int c = column<TPR>(eights, v, 0, t, width);
-  if (vec) return c < n ? fetch_eight<T>(row + c, true, 8, lo, hi) : Eight<T>{};  // n is a multiple of 8
+  if (A == kVec) return c < n ? fetch_eight<T>(row + c, true, 8, lo, hi) : Eight<T>{};  // n is a multiple of 8
+  if (A == kPhase) {
+    Eight<T> o = {};
+    // in 16 bits a row's ends are loaded with their neighbours and settled later, but for
+    // the matrix's own ends (value by value 307 us for 201 backward at 65536 x 1659);
+    // fp32 is 5% faster value by value
+    const T *p = row + c;
+    if (c < n && ((c >= lead && c + 8 <= n) || (sizeof(T) == 2 && p >= lo && p + 8 <= hi))) {
+      o = fetch_eight<T>(p, true, 8, lo, hi);
+    } else if (c < n) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const bool in = c + q >= lead && c + q < n;
+        if (sizeof(T) == 4) o.r[q] = load_if32(p + q, in);
+        else o.r[q >> 1] |= (uint32_t)load_if16(p + q, in) << (16 * (q & 1));
+      }
+    }
+    return o;
+  }
   if (sizeof(T) == 2) return fetch_eight<T>(row + c, false, min(8, n - c), lo, hi);
   // predicated loads without branches, so that all are under way at once
   Eight<T> o;
@@ -93,11 +124,21 @@ __device__ __forceinline__ Eight<T> load_raw(const T *row, int eights, bool vec,
   for (int q = 0; q < 8; ++q, p += st) o.r[q] = load_if32(p, c + q * st < n);
   return o;
 }
-template <int TPR, typename T>
-__device__ __forceinline__ void settle_raw(Eight<T> &o, const T *row, bool vec, int v, int t, int n, const void *lo,
+template <int TPR, int A, typename T>
+__device__ __forceinline__ void settle_raw(Eight<T> &o, const T *row, int v, int t, int lead, int n, const void *lo,
                                            const void *hi, int width = TPR) {
-  if (vec || sizeof(T) == 4) return;
+  if (A == kVec || sizeof(T) == 4) return;
   const int c = column<TPR>(1, v, 0, t, width);
+  if (A == kPhase) {  // zeros for the neighbouring rows' values
+    if (c < lead || c + 8 > n) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const bool in = c + q >= lead && c + q < n;
+        o.r[q >> 1] &= in ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
+      }
+    }
+    return;
+  }
   settle_eight<T>(o, row + c, false, min(8, n - c), lo, hi);
 }
 // x, which may be a checkpoint: then the codes as numbers of T, exactly, and
@@ -125,12 +166,18 @@ __device__ __forceinline__ Eight<T> load_held(const Rows &x, int64_t i, int v, i
   }
   return o;
 }
-template <int TPR, typename T>
-__device__ __forceinline__ void store_row(T *row, int eights, bool vec, int v, int t, int n, const float2 (&p)[4], int width = TPR) {
+template <int TPR, int A, typename T>
+__device__ __forceinline__ void store_row(T *row, int eights, int v, int t, int lead, int n, const float2 (&p)[4], int width = TPR) {
   const float o[8] = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
   const int c = column<TPR>(eights, v, 0, t, width);
-  if (vec) {
+  if (A == kVec || (A == kPhase && c >= lead && c + 8 <= n)) {
     if (c < n) store8(row, c, TypeCode<T>::code, 1, 8, o);
+    return;
+  }
+  if (A == kPhase) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (c + q >= lead && c + q < n) row[c + q] = from_f32<T>(o[q]);
     return;
   }
   if (sizeof(T) == 2) {  // a group's lanes of a warp walk a row in step
@@ -148,8 +195,8 @@ __device__ __forceinline__ void store_row(T *row, int eights, bool vec, int v, i
     if (c + q * st < n) row[c + q * st] = from_f32<T>(o[q]);
 }
 // eight of the weights (or biases) as a thread's columns need them
-template <int TPR>
-__device__ __forceinline__ void load_w(const void *p, int dtype, float none, int eights, bool vec, int v, int t, int n,
+template <int TPR, int A>
+__device__ __forceinline__ void load_w(const void *p, int dtype, float none, int eights, int v, int t, int lead, int n,
                                        float2 (&w)[4], int width = TPR) {
   float o[8];
   const int c = column<TPR>(eights, v, 0, t, width);
@@ -157,8 +204,11 @@ __device__ __forceinline__ void load_w(const void *p, int dtype, float none, int
   if (!p) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) o[q] = none;
-  } else if (vec) {  // known when compiled
+  } else if (A == kVec) {
     load8(p, c < n ? c : 0, dtype, 1, 8, o);
+  } else if (A == kPhase) {  // once a block
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = c + q >= lead && c + q < n ? load_any(p, c + q - lead, dtype) : 0.0f;
   } else if (eights && c + 8 <= n && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {  // rows end anywhere, the weights begin well
     load8(p, c, dtype, 1, 8, o);
   } else if (dtype == NR_F32) {  // one test of the type, all loads under way at once
@@ -235,39 +285,41 @@ __device__ __forceinline__ void block_sums(float (&v)[K], BlockSums<K> &S, int t
 // R rows from i on of a group of TPR threads (0: the block), V eights a thread:
 // centred, with their means and reciprocal deviations, then written. Rows from
 // m on are skipped (they hold zeros).
-template <int TPR, int V, int R, bool VEC, typename T>
+template <int TPR, int V, int R, int A, typename T>
 struct Forward {
   // Rows of 16 bits are loaded a turn ahead, so that loads are under way during the
   // sums (2^20 x 128: 105 -> 86 us, 65536 x 4096: 330 -> 280 us; backward, where a
   // row's registers are twice as many, half the rows a turn and the next ones
   // ahead took 573 us for 450 at 262144 x 1536).
-  static constexpr bool kAhead = VEC && sizeof(T) == 2;
+  static constexpr bool kAhead = A != kAny && sizeof(T) == 2;
+  static constexpr int kStep = kStepOf<A, T>;
+  int lead = 0;
   Eight<T> raw[R][V];
   float2 x[R][V][4];
   float mean[R], rstd[R];
 
   __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int width) {
-    const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
+    const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld - lead;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        raw[r][v] = i + r < N.m ? load_raw<TPR, T>(p + r * N.x.ld, eights, VEC, v, t, (int)N.n, N.x.p, N.x_end, width)
-                                : Eight<T>{};
+        raw[r][v] = i + r * kStep < N.m ? load_raw<TPR, A, T>(p + r * kStep * N.x.ld, eights, v, t, lead, (int)N.n + lead, N.x.p, N.x_end, width)
+                                        : Eight<T>{};
   }
   // rows i on, `next` the turn after's
   template <typename Sums>
   __device__ __forceinline__ void statistics(const Norm &N, int64_t i, int64_t next, int t, int eights, int width, Sums sums) {
-    const int n = (int)N.n;
-    const float inv = 1.0f / (float)n;
-    if (!N.x.scale) {
+    const int n = (int)N.n + lead;
+    const float inv = 1.0f / (float)(int)N.n;
+    if (A == kPhase || !N.x.scale) {
       const T *p = static_cast<const T *>(N.x.p) + i * N.x.ld;
       if (!kAhead) load(N, i, t, eights, width);
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          if (i + r < N.m) settle_raw<TPR, T>(raw[r][v], p + r * N.x.ld, VEC, v, t, n, N.x.p, N.x_end, width);
+          if (i + r * kStep < N.m) settle_raw<TPR, A, T>(raw[r][v], p + r * kStep * N.x.ld, v, t, lead, n, N.x.p, N.x_end, width);
 #pragma unroll
           for (int q = 0; q < 4; ++q) x[r][v][q] = pair_of<T>(raw[r][v], q);
         }
@@ -305,11 +357,12 @@ struct Forward {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float2 d = add2(x[r][v][q], both(-mean[r]));
-          if (VEC) {
+          if (A == kVec) {
             if (!in) d = both(0.0f);
           } else {
-            if (column<TPR>(eights, v, 2 * q, t, width) >= n) d.x = 0.0f;
-            if (column<TPR>(eights, v, 2 * q + 1, t, width) >= n) d.y = 0.0f;
+            const int c0 = column<TPR>(eights, v, 2 * q, t, width), c1 = column<TPR>(eights, v, 2 * q + 1, t, width);
+            if (c0 >= n || (A == kPhase && c0 < lead)) d.x = 0.0f;
+            if (c1 >= n || (A == kPhase && c1 < lead)) d.y = 0.0f;
           }
           x[r][v][q] = d;
           s = fma2(d, d, s);
@@ -324,47 +377,48 @@ struct Forward {
 
   __device__ __forceinline__ void write(const Norm &N, int64_t i, int v, int t, int eights, int width,
                                         const float2 (&w)[4], const float2 (&b)[4]) {
-    T *y = static_cast<T *>(N.y) + i * N.y_ld;
+    T *y = static_cast<T *>(N.y) + i * N.y_ld - lead;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (i + r >= N.m) break;
+      if (i + r * kStep >= N.m) break;
       float2 o[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) o[q] = fma2(mul2(x[r][v][q], both(rstd[r])), w[q], b[q]);
-      store_row<TPR, T>(y + r * N.y_ld, eights, VEC, v, t, (int)N.n, o, width);
+      store_row<TPR, A, T>(y + r * kStep * N.y_ld, eights, v, t, lead, (int)N.n + lead, o, width);
     }
   }
   __device__ __forceinline__ void write_statistics(const Norm &N, int64_t i) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (i + r < N.m) {
-        N.mean[i + r] = mean[r];
-        N.rstd[i + r] = rstd[r];
+      if (i + r * kStep < N.m) {
+        N.mean[i + r * kStep] = mean[r];
+        N.rstd[i + r * kStep] = rstd[r];
       }
   }
 };
 
 // The same for the backward pass: x and dy stay as they lie in memory, and are
 // converted twice.
-template <int TPR, int V, int R, bool VEC, typename T>
+template <int TPR, int V, int R, int A, typename T>
 struct Backward {
+  static constexpr int kStep = kStepOf<A, T>;
   Eight<T> x[R][V], dy[R][V];
   float scale[R][V], shift[R], rstd[R];  // xh = x scale + shift
   float s[2 * R];                        // sum g, sum g xh of the thread's columns, then of the rows
 
-  __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int width) {
-    const int n = (int)N.n;
-    const T *pd = static_cast<const T *>(N.dy) + i * N.dy_ld, *px = static_cast<const T *>(N.x.p) + i * N.x.ld;
+  __device__ __forceinline__ void load(const Norm &N, int64_t i, int t, int eights, int lead, int width) {
+    const int n = (int)N.n + lead;
+    const T *pd = static_cast<const T *>(N.dy) + i * N.dy_ld - lead, *px = static_cast<const T *>(N.x.p) + i * N.x.ld - lead;
     // the residual's gradient into L2 while the sums are made, a line for the eight
     // threads that read it (65536 x 1536 in bf16: 180 -> 162 us; fp32 gained nothing)
-    if (VEC && sizeof(T) == 2 && N.dres && (t & 7) == 0) {
-      const T *pr = static_cast<const T *>(N.dres) + i * N.dres_ld;
+    if (A != kAny && sizeof(T) == 2 && N.dres && (t & 7) == 0) {
+      const T *pr = static_cast<const T *>(N.dres) + i * N.dres_ld - lead;
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int c = column<TPR>(1, v, 0, t, width);
-          if (i + r < N.m && c < n) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(pr + r * N.dres_ld + c));
+          if (i + r * kStep < N.m && c < n) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(pr + r * kStep * N.dres_ld + c));
         }
     }
     // one branch around all loads, so that they are under way together; rows past
@@ -373,8 +427,10 @@ struct Backward {
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        dy[r][v] = i + r < N.m ? load_raw<TPR, T>(pd + r * N.dy_ld, eights, VEC, v, t, n, N.dy, N.dy_end, width) : Eight<T>{};
-    if (N.x.scale) {
+        dy[r][v] = i + r * kStep < N.m
+                       ? load_raw<TPR, A, T>(pd + r * kStep * N.dy_ld, eights, v, t, lead, n, N.dy, N.dy_end, width)
+                       : Eight<T>{};
+    if (A != kPhase && N.x.scale) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -384,24 +440,28 @@ struct Backward {
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          x[r][v] = i + r < N.m ? load_raw<TPR, T>(px + r * N.x.ld, eights, VEC, v, t, n, N.x.p, N.x_end, width) : Eight<T>{};
+          x[r][v] = i + r * kStep < N.m
+                        ? load_raw<TPR, A, T>(px + r * kStep * N.x.ld, eights, v, t, lead, n, N.x.p, N.x_end, width)
+                        : Eight<T>{};
           scale[r][v] = 1.0f;
         }
     }
-    if (!VEC) {
+    if (A != kVec) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          if (i + r >= N.m) break;
-          settle_raw<TPR, T>(dy[r][v], pd + r * N.dy_ld, VEC, v, t, n, N.dy, N.dy_end, width);
-          if (!N.x.scale) settle_raw<TPR, T>(x[r][v], px + r * N.x.ld, VEC, v, t, n, N.x.p, N.x_end, width);
+          if (i + r * kStep >= N.m) break;
+          settle_raw<TPR, A, T>(dy[r][v], pd + r * kStep * N.dy_ld, v, t, lead, n, N.dy, N.dy_end, width);
+          if (A == kPhase || !N.x.scale)
+            settle_raw<TPR, A, T>(x[r][v], px + r * kStep * N.x.ld, v, t, lead, n, N.x.p, N.x_end, width);
         }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      shift[r] = i + r < N.m ? N.mean[i + r] : 0.0f;
-      rstd[r] = i + r < N.m ? N.rstd[i + r] : 0.0f;
+      const int64_t j = i + r * kStep;
+      shift[r] = j < N.m ? N.mean[j] : 0.0f;
+      rstd[r] = j < N.m ? N.rstd[j] : 0.0f;
       s[2 * r] = s[2 * r + 1] = 0.0f;
     }
 #pragma unroll
@@ -429,14 +489,15 @@ struct Backward {
       s[2 * r + 1] += s2.x + s2.y;
     }
   }
-  __device__ __forceinline__ void write(const Norm &N, int64_t i, int v, int t, int eights, int width,
+  __device__ __forceinline__ void write(const Norm &N, int64_t i, int v, int t, int eights, int lead, int width,
                                         const float2 (&w)[4]) {
     const float inv = 1.0f / (float)(int)N.n;
-    const T *res = static_cast<const T *>(N.dres) + i * N.dres_ld;
-    T *dx = static_cast<T *>(N.dx) + i * N.dx_ld;
+    const int n = (int)N.n + lead;
+    const T *res = static_cast<const T *>(N.dres) + i * N.dres_ld - lead;
+    T *dx = static_cast<T *>(N.dx) + i * N.dx_ld - lead;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (i + r >= N.m) break;
+      if (i + r * kStep >= N.m) break;
       forget(x[r][v]);
       forget(dy[r][v]);
       const float2 m1 = both(-s[2 * r] * inv * rstd[r]), m2 = both(-s[2 * r + 1] * inv * rstd[r]);
@@ -447,13 +508,27 @@ struct Backward {
         o[q] = fma2(xh, m2, fma2(mul2(pair_of<T>(dy[r][v], q), w[q]), both(rstd[r]), m1));
       }
       if (N.dres) {
-        Eight<T> rr = load_raw<TPR, T>(res + r * N.dres_ld, eights, VEC, v, t, (int)N.n, N.dres, N.dres_end, width);
-        settle_raw<TPR, T>(rr, res + r * N.dres_ld, VEC, v, t, (int)N.n, N.dres, N.dres_end, width);
+        Eight<T> rr = load_raw<TPR, A, T>(res + r * kStep * N.dres_ld, eights, v, t, lead, n, N.dres, N.dres_end, width);
+        settle_raw<TPR, A, T>(rr, res + r * kStep * N.dres_ld, v, t, lead, n, N.dres, N.dres_end, width);
 #pragma unroll
         for (int q = 0; q < 4; ++q) o[q] = add2(o[q], pair_of<T>(rr, q));
       }
-      store_row<TPR, T>(dx + r * N.dx_ld, eights, VEC, v, t, (int)N.n, o, width);
+      store_row<TPR, A, T>(dx + r * kStep * N.dx_ld, eights, v, t, lead, n, o, width);
     }
+  }
+};
+
+// The rows of a block: kStep phases of blocks, each with its rows; `unit` rows a turn.
+template <int A, typename T>
+struct Walk {
+  int64_t first, stride;  // of a block
+  int lead;
+  __device__ __forceinline__ Walk(const Norm &N, const void *p, int64_t ld, int unit) {
+    constexpr int kStep = kStepOf<A, T>;
+    const int phase = kStep > 1 ? blockIdx.x % kStep : 0;
+    first = phase + (int64_t)(blockIdx.x / kStep) * unit * kStep;
+    stride = (int64_t)(gridDim.x / kStep) * unit * kStep;
+    lead = kStep > 1 ? (int)((reinterpret_cast<uintptr_t>(p) + (uintptr_t)(phase * ld) * sizeof(T)) & 15) / (int)sizeof(T) : 0;
   }
 };
 
@@ -461,28 +536,30 @@ struct Backward {
 // Blocks of 128: groups of TPR lanes hold R rows each, V eights of them a thread.
 constexpr int kWarpThreads = 128;
 
-template <int TPR, int V, bool VEC, typename T>
+template <int TPR, int V, int A, typename T>
 __global__ void __launch_bounds__(kWarpThreads, 4) warp_forward_kernel(const Norm N) {
   constexpr int R = V == 6 ? 1 : V == 3 ? 2 : 4, kGroups = kWarpThreads / TPR;
-  const int t = threadIdx.x % TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
+  const Walk<A, T> W(N, N.x.p, N.x.ld, kGroups * R);
+  const int t = threadIdx.x % TPR, lead = W.lead, n = (int)N.n + lead, eights = A != kAny ? 1 : N.eights;
+  const int own = threadIdx.x / TPR * R * kStepOf<A, T>;  // the group's first row in the block's
   float2 w[4], b[4];  // V = 1: a thread's own, kept
   if (V == 1) {
-    load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, 0, t, n, w);
-    load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, VEC, 0, t, n, b);
+    load_w<TPR, A>(N.weight, N.w_dtype, 1.0f, eights, 0, t, lead, n, w);
+    load_w<TPR, A>(N.bias, N.w_dtype, 0.0f, eights, 0, t, lead, n, b);
   }
-  const int64_t stride = (int64_t)gridDim.x * kGroups * R;
-  Forward<TPR, V, R, VEC, T> F;
-  if (F.kAhead && !N.x.scale) F.load(N, (int64_t)blockIdx.x * kGroups * R + threadIdx.x / TPR * R, t, eights, TPR);
+  Forward<TPR, V, R, A, T> F;
+  F.lead = lead;
+  if (F.kAhead && (A == kPhase || !N.x.scale)) F.load(N, W.first + own, t, eights, TPR);
   // a block's groups take the same number of turns, so that shuffles are complete
-  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += stride) {
-    const int64_t i = i0 + threadIdx.x / TPR * R;
-    F.statistics(N, i, i + stride, t, eights, TPR, [](float(&v)[R]) { lane_sums<TPR, R>(v); });
+  for (int64_t i0 = W.first; i0 < N.m; i0 += W.stride) {
+    const int64_t i = i0 + own;
+    F.statistics(N, i, i + W.stride, t, eights, TPR, [](float(&v)[R]) { lane_sums<TPR, R>(v); });
     if (V > 1) forget();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (V > 1) {
-        load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w);
-        load_w<TPR>(N.bias, N.w_dtype, 0.0f, eights, VEC, v, t, n, b);
+        load_w<TPR, A>(N.weight, N.w_dtype, 1.0f, eights, v, t, lead, n, w);
+        load_w<TPR, A>(N.bias, N.w_dtype, 0.0f, eights, v, t, lead, n, b);
       }
       F.write(N, i, v, t, eights, TPR, w, b);
     }
@@ -491,20 +568,22 @@ __global__ void __launch_bounds__(kWarpThreads, 4) warp_forward_kernel(const Nor
 }
 
 // Up to 256 columns: V = 1, four rows a group (two in fp32).
-template <int TPR, bool VEC, typename T>
+template <int TPR, int A, typename T>
 __global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const Norm N) {
   constexpr int R = sizeof(T) == 4 ? 2 : 4, kGroups = kWarpThreads / TPR;
   __shared__ float sums[2][TPR * 8];
-  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, n = (int)N.n, eights = VEC ? 1 : N.eights;
+  const Walk<A, T> W(N, N.dy, N.dy_ld, kGroups * R);
+  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, lead = W.lead, n = (int)N.n + lead;
+  const int eights = A != kAny ? 1 : N.eights;
   float2 w[4], dw[4] = {}, db[4] = {};
-  load_w<TPR>(N.weight, N.w_dtype, 1.0f, eights, VEC, 0, t, n, w);
-  for (int64_t i0 = (int64_t)blockIdx.x * kGroups * R; i0 < N.m; i0 += (int64_t)gridDim.x * kGroups * R) {
-    const int64_t i = i0 + group * R;
-    Backward<TPR, 1, R, VEC, T> G;
-    G.load(N, i, t, eights, TPR);
+  load_w<TPR, A>(N.weight, N.w_dtype, 1.0f, eights, 0, t, lead, n, w);
+  for (int64_t i0 = W.first; i0 < N.m; i0 += W.stride) {
+    const int64_t i = i0 + group * R * kStepOf<A, T>;
+    Backward<TPR, 1, R, A, T> G;
+    G.load(N, i, t, eights, lead, TPR);
     G.add(0, w, dw, db);
     lane_sums<TPR, 2 * R>(G.s);
-    G.write(N, i, 0, t, eights, TPR, w);
+    G.write(N, i, 0, t, eights, lead, TPR, w);
   }
   grid_launch();
   if (!N.parts) return;
@@ -521,9 +600,9 @@ __global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const No
         }
         sums[0][t * 8 + q] = a;
         sums[1][t * 8 + q] = e;
-        if (g + 1 == kGroups && c < n) {
-          part[c] = a;
-          part[n + c] = e;
+        if (g + 1 == kGroups && c >= lead && c < n) {
+          part[c - lead] = a;
+          part[N.n + c - lead] = e;
         }
       }
     }
@@ -533,21 +612,28 @@ __global__ void __launch_bounds__(kWarpThreads, 4) warp_backward_kernel(const No
 
 // ------------------------------------------------------------ a row in a block
 // The block has just the threads that a row's eights need; R rows at a time.
-template <int V, int R, int THREADS, bool VEC, typename T>
+template <int V, int R, int THREADS, int A, typename T>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) block_forward_kernel(const Norm N) {
   __shared__ BlockSums<R> S;
-  const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
+  const Walk<A, T> W(N, N.x.p, N.x.ld, R);
+  const int t = threadIdx.x, lead = W.lead, n = (int)N.n + lead, eights = A != kAny ? 1 : N.eights, width = blockDim.x;
+  float2 w[4], b[4];  // kPhase: a thread's own, kept
+  if (A == kPhase) {
+    load_w<0, A>(N.weight, N.w_dtype, 1.0f, eights, 0, t, lead, n, w, width);
+    load_w<0, A>(N.bias, N.w_dtype, 0.0f, eights, 0, t, lead, n, b, width);
+  }
   int turn = 0;
-  const int64_t stride = (int64_t)gridDim.x * R;
-  Forward<0, V, R, VEC, T> F;
-  if (F.kAhead && !N.x.scale) F.load(N, (int64_t)blockIdx.x * R, t, eights, width);
-  for (int64_t i = (int64_t)blockIdx.x * R; i < N.m; i += stride) {
-    F.statistics(N, i, i + stride, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++, t, width, 0); });
+  Forward<0, V, R, A, T> F;
+  F.lead = lead;
+  if (F.kAhead && (A == kPhase || !N.x.scale)) F.load(N, W.first, t, eights, width);
+  for (int64_t i = W.first; i < N.m; i += W.stride) {
+    F.statistics(N, i, i + W.stride, t, eights, width, [&](float(&v)[R]) { block_sums<R>(v, S, turn++, t, width, 0); });
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      float2 w[4], b[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
-      load_w<0>(N.bias, N.w_dtype, 0.0f, eights, VEC, v, t, n, b, width);
+      if (A != kPhase) {
+        load_w<0, A>(N.weight, N.w_dtype, 1.0f, eights, v, t, lead, n, w, width);
+        load_w<0, A>(N.bias, N.w_dtype, 0.0f, eights, v, t, lead, n, b, width);
+      }
       F.write(N, i, v, t, eights, width, w, b);
     }
     if (N.mean && t == 0) F.write_statistics(N, i);
@@ -556,30 +642,36 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : V == 4 ? 1 : 2) 
 
 // Backward: with THREADS 384 blockDim.y groups of blockDim.x threads, R rows each,
 // so that short rows leave few blocks' sums to add; the groups' are added in order.
-template <int V, int R, int THREADS, bool VEC, typename T>
+template <int V, int R, int THREADS, int A, typename T>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ? 2 : 1) block_backward_kernel(const Norm N) {
   __shared__ BlockSums<2 * R> S;
   extern __shared__ float sums[];  // [2][n], with several groups
-  const int t = threadIdx.x, n = (int)N.n, eights = VEC ? 1 : N.eights, width = blockDim.x;
   const int group = THREADS == 384 ? threadIdx.y : 0, groups = THREADS == 384 ? blockDim.y : 1;
+  const Walk<A, T> W(N, N.dy, N.dy_ld, groups * R);
+  const int t = threadIdx.x, lead = W.lead, n = (int)N.n + lead, eights = A != kAny ? 1 : N.eights, width = blockDim.x;
+  float2 own[A == kPhase ? V : 1][4];  // weights, kept
+  if (A == kPhase) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_w<0, A>(N.weight, N.w_dtype, 1.0f, eights, v, t, lead, n, own[A == kPhase ? v : 0], width);
+  }
   float2 dw[V][4] = {}, db[V][4] = {};
   int turn = 0;
-  for (int64_t i = ((int64_t)blockIdx.x * groups + group) * R; i < N.m; i += (int64_t)gridDim.x * groups * R) {
-    Backward<0, V, R, VEC, T> G;
-    G.load(N, i, t, eights, width);
+  for (int64_t i = W.first + group * R * kStepOf<A, T>; i < N.m; i += W.stride) {
+    Backward<0, V, R, A, T> G;
+    G.load(N, i, t, eights, lead, width);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      float2 w[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
+      float2(&w)[4] = own[A == kPhase ? v : 0];
+      if (A != kPhase) load_w<0, A>(N.weight, N.w_dtype, 1.0f, eights, v, t, lead, n, w, width);
       G.add(v, w, dw[v], db[v]);
     }
     block_sums<2 * R>(G.s, S, turn++, t, width, group);
     forget();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      float2 w[4];
-      load_w<0>(N.weight, N.w_dtype, 1.0f, eights, VEC, v, t, n, w, width);
-      G.write(N, i, v, t, eights, width, w);
+      float2(&w)[4] = own[A == kPhase ? v : 0];
+      if (A != kPhase) load_w<0, A>(N.weight, N.w_dtype, 1.0f, eights, v, t, lead, n, w, width);
+      G.write(N, i, v, t, eights, lead, width, w);
     }
   }
   grid_launch();
@@ -591,16 +683,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : THREADS == 384 ?
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const int c = column<0>(eights, v, q, t, width);
-          if (c >= n) continue;
+          const int c = column<0>(eights, v, q, t, width) - lead;
+          if (c < 0 || c >= (int)N.n) continue;
           float a = q & 1 ? dw[v][q >> 1].y : dw[v][q >> 1].x, e = q & 1 ? db[v][q >> 1].y : db[v][q >> 1].x;
           if (g > 0) {
             a += sums[c];
-            e += sums[n + c];
+            e += sums[N.n + c];
           }
           float *to = g + 1 < groups ? sums : part;
           to[c] = a;
-          to[n + c] = e;
+          to[N.n + c] = e;
         }
     }
     if (groups > 1) __syncthreads();
@@ -741,9 +833,16 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
   else
     vec = vec && vec_ok(a->y, a->y_ld, dt);
   vec = vec && vec_ok(a->weight, 8, a->w_dtype) && vec_ok(a->bias, 8, a->w_dtype);
-  N.vec = vec;
-  N.eights = vec || a->x_scale || dt != NR_F32;
-  const int64_t e = (int64_t)type_bytes(dt);
+  const int64_t e = (int64_t)type_bytes(dt), step = 16 / e;
+  const auto alike = [&](const void *p, int64_t ld) {
+    return ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(a->x)) & 15) == 0 && (ld - a->x_ld) % step == 0;
+  };
+  const bool phase = !vec && !a->x_scale && a->n <= (backward ? 8192 : 4096) - step &&
+                     (backward ? alike(a->dy, a->dy_ld) && alike(a->dx, a->dx_ld) &&
+                                     (!a->residual_grad || alike(a->residual_grad, a->residual_grad_ld))
+                               : alike(a->y, a->y_ld));
+  N.lie = vec ? kVec : phase ? kPhase : kAny;
+  N.eights = vec || phase || a->x_scale || dt != NR_F32;
   N.x_end = static_cast<const char *>(a->x) + ((a->m - 1) * a->x_ld + a->n) * e;
   N.dy_end = static_cast<const char *>(a->dy) + ((a->m - 1) * a->dy_ld + a->n) * e;
   N.dres_end = static_cast<const char *>(a->residual_grad) + ((a->m - 1) * a->residual_grad_ld + a->n) * e;
@@ -759,7 +858,9 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
 struct Shape {
   int tpr, v, threads, groups;  // threads a row's group, groups a block
 };
-Shape shape_of(int64_t n, bool vec, bool small, bool backward) {
+Shape shape_of(const Norm &N, bool small, bool backward) {
+  const bool vec = N.lie == kVec;
+  const int64_t n = N.n + (N.lie == kPhase ? (small ? 7 : 3) : 0);  // with the values before a row
   if (n <= 256) return {n <= 64 ? 8 : n <= 128 ? 16 : 32, 1, kWarpThreads, 1};
   if (!backward && vec && n <= 768) return {32, 3, kWarpThreads, 1};
   if (!backward && vec && n <= 1536) return {32, 6, kWarpThreads, 1};
@@ -778,7 +879,8 @@ Shape shape_of(int64_t n, bool vec, bool small, bool backward) {
 
 // Blocks of a persistent grid: those the registers allow at once, by sizes alone,
 // so that the order of the parameters' sums is fixed.
-int block_count(const Shape &s, int64_t m, bool backward, bool vec, int sms) {
+int block_count(const Shape &s, const Norm &N, bool small, bool backward, int sms) {
+  const bool vec = N.lie != kAny;
   int per_sm, rows = s.groups;
   if (s.tpr) {
     per_sm = 4;
@@ -789,49 +891,51 @@ int block_count(const Shape &s, int64_t m, bool backward, bool vec, int sms) {
     const int held = !backward ? s.threads <= 256 ? 768 : s.v < 4 ? 1024 : 512 : s.v == 2 && !vec ? 580 : 512;
     per_sm = held / s.threads;
   }
-  const int64_t need = ceil_div(m, rows), most = (int64_t)sms * per_sm;
+  const int64_t step = N.lie == kPhase ? small ? 8 : 4 : 1;
+  const int64_t need = round_up(ceil_div(N.m, rows), step), most = (int64_t)sms * per_sm / step * step;
   return (int)(need < most ? need : most);
 }
 
 // rows at a time of a block with one eight a thread: what 80 registers hold
-template <bool VEC, typename T>
-constexpr int block_rows() { return VEC && sizeof(T) == 2 ? 4 : 2; }
+template <int A, typename T>
+constexpr int block_rows() { return A == kVec && sizeof(T) == 2 ? 4 : 2; }
 
-template <bool VEC, typename T>
+template <int A, typename T>
 cudaError_t forward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
   const int th = s.threads;
-  if (s.tpr == 8) warp_forward_kernel<8, 1, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr == 16) warp_forward_kernel<16, 1, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr && s.v == 1) warp_forward_kernel<32, 1, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr && s.v == 3) warp_forward_kernel<32, 3, true, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr) warp_forward_kernel<32, 6, true, T><<<blocks, th, 0, st>>>(N);
-  else if (s.v == 1 && th <= 256) block_forward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.v == 1) block_forward_kernel<1, 2, 512, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (VEC && s.v == 2 && th <= 256) block_forward_kernel<2, sizeof(T) == 2 ? 2 : 1, 256, true, T><<<blocks, th, 0, st>>>(N);
-  else if (VEC && s.v == 4 && th <= 256) block_forward_kernel<4, 1, 256, true, T><<<blocks, th, 0, st>>>(N);
-  else if (s.v == 2) block_forward_kernel<2, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
-  else block_forward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+  if (s.tpr == 8) warp_forward_kernel<8, 1, A, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_forward_kernel<16, 1, A, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr && s.v == 1) warp_forward_kernel<32, 1, A, T><<<blocks, th, 0, st>>>(N);
+  else if (s.v == 1 && th <= 256) block_forward_kernel<1, block_rows<A, T>(), 256, A, T><<<blocks, th, 0, st>>>(N);
+  else if (A != kVec && s.v == 1) block_forward_kernel<1, 2, 512, A == kVec ? kAny : A, T><<<blocks, th, 0, st>>>(N);
+  else if (A == kVec && s.tpr && s.v == 3) warp_forward_kernel<32, 3, kVec, T><<<blocks, th, 0, st>>>(N);
+  else if (A == kVec && s.tpr) warp_forward_kernel<32, 6, kVec, T><<<blocks, th, 0, st>>>(N);
+  else if (A == kVec && s.v == 2 && th <= 256)
+    block_forward_kernel<2, sizeof(T) == 2 ? 2 : 1, 256, kVec, T><<<blocks, th, 0, st>>>(N);
+  else if (A == kVec && s.v == 4 && th <= 256) block_forward_kernel<4, 1, 256, kVec, T><<<blocks, th, 0, st>>>(N);
+  else if (A != kPhase && s.v == 2) block_forward_kernel<2, 1, 512, A == kPhase ? kAny : A, T><<<blocks, th, 0, st>>>(N);
+  else if (A != kPhase) block_forward_kernel<4, 1, 512, A == kPhase ? kAny : A, T><<<blocks, th, 0, st>>>(N);
   return cudaGetLastError();
 }
-template <bool VEC, typename T>
+template <int A, typename T>
 cudaError_t backward_typed(const Norm &N, const Shape &s, int blocks, cudaStream_t st) {
   const int th = s.threads;
-  if (s.tpr == 8) warp_backward_kernel<8, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr == 16) warp_backward_kernel<16, VEC, T><<<blocks, th, 0, st>>>(N);
-  else if (s.tpr) warp_backward_kernel<32, VEC, T><<<blocks, th, 0, st>>>(N);
+  if (s.tpr == 8) warp_backward_kernel<8, A, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr == 16) warp_backward_kernel<16, A, T><<<blocks, th, 0, st>>>(N);
+  else if (s.tpr) warp_backward_kernel<32, A, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1 && s.groups == 1)
-    block_backward_kernel<1, block_rows<VEC, T>(), 256, VEC, T><<<blocks, th, 0, st>>>(N);
+    block_backward_kernel<1, block_rows<A, T>(), 256, A, T><<<blocks, th, 0, st>>>(N);
   else if (s.v == 1)
-    block_backward_kernel<1, block_rows<VEC, T>(), 384, VEC, T>
-        <<<blocks, dim3(th, s.groups), (size_t)N.n * 8, st>>>(N);
-  else if (s.v == 2) block_backward_kernel<2, VEC && sizeof(T) == 2 ? 2 : 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
-  else block_backward_kernel<4, 1, 512, VEC, T><<<blocks, th, 0, st>>>(N);
+    block_backward_kernel<1, block_rows<A, T>(), 384, A, T><<<blocks, dim3(th, s.groups), (size_t)N.n * 8, st>>>(N);
+  else if (s.v == 2) block_backward_kernel<2, A == kVec && sizeof(T) == 2 ? 2 : 1, 512, A, T><<<blocks, th, 0, st>>>(N);
+  else if (A != kPhase) block_backward_kernel<4, 1, 512, A == kPhase ? kAny : A, T><<<blocks, th, 0, st>>>(N);
   return cudaGetLastError();
 }
 template <typename T>
 cudaError_t launch_typed(const Norm &N, const Shape &s, bool backward, int blocks, cudaStream_t st) {
-  if (backward) return N.vec ? backward_typed<true, T>(N, s, blocks, st) : backward_typed<false, T>(N, s, blocks, st);
-  return N.vec ? forward_typed<true, T>(N, s, blocks, st) : forward_typed<false, T>(N, s, blocks, st);
+  if (N.lie == kVec) return backward ? backward_typed<kVec, T>(N, s, blocks, st) : forward_typed<kVec, T>(N, s, blocks, st);
+  if (N.lie == kPhase) return backward ? backward_typed<kPhase, T>(N, s, blocks, st) : forward_typed<kPhase, T>(N, s, blocks, st);
+  return backward ? backward_typed<kAny, T>(N, s, blocks, st) : forward_typed<kAny, T>(N, s, blocks, st);
 }
 cudaError_t launch_any(const Norm &N, const Shape &s, bool backward, int64_t dtype, int blocks, cudaStream_t st) {
   if (dtype == NR_F32) return launch_typed<float>(N, s, backward, blocks, st);
@@ -849,10 +953,10 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
   if (!g.ok) return NR_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Norm N = norm_of(a, false);
-  const Shape sh = shape_of(a->n, N.vec, a->dtype != NR_F32, false);
+  const Shape sh = shape_of(N, a->dtype != NR_F32, false);
   cudaError_t e;
   if (sh.threads) {
-    e = launch_any(N, sh, false, a->dtype, block_count(sh, a->m, false, N.vec, nr_ops_sms(device)), s);
+    e = launch_any(N, sh, false, a->dtype, block_count(sh, N, a->dtype != NR_F32, false, nr_ops_sms(device)), s);
   } else {
     long_forward_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);
     e = cudaGetLastError();
@@ -863,9 +967,9 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
 extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int device) {
   if (!valid(a, true)) return -1;
   if (a->m == 0 || !a->dweight) return 0;
-  const bool vec = norm_of(a, true).vec;
-  const Shape sh = shape_of(a->n, vec, a->dtype != NR_F32, true);
-  const int64_t blocks = sh.threads ? block_count(sh, a->m, true, vec, nr_ops_sms(device)) : kLongParts;
+  const Norm N = norm_of(a, true);
+  const Shape sh = shape_of(N, a->dtype != NR_F32, true);
+  const int64_t blocks = sh.threads ? block_count(sh, N, a->dtype != NR_F32, true, nr_ops_sms(device)) : kLongParts;
   return round_up(blocks * 2 * a->n * 4, 256);
 }
 
@@ -886,10 +990,10 @@ extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, 
   }
   Norm N = norm_of(a, true);
   N.parts = a->dweight ? static_cast<float *>(ws) : nullptr;
-  const Shape sh = shape_of(a->n, N.vec, a->dtype != NR_F32, true);
+  const Shape sh = shape_of(N, a->dtype != NR_F32, true);
   int parts = kLongParts;
   if (sh.threads) {
-    parts = block_count(sh, a->m, true, N.vec, nr_ops_sms(device));
+    parts = block_count(sh, N, a->dtype != NR_F32, true, nr_ops_sms(device));
     e = launch_any(N, sh, true, a->dtype, parts, s);
   } else {
     long_dx_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);

@@ -276,6 +276,72 @@ def test_layer_norm(ops, i, shape, dtype):
         assert only[1] is None and only[2] is None and torch.equal(only[0], dx)
 
 
+@pytest.mark.parametrize("shape", [(1, 1), (9, 3), (2, 9), (7, 57), (8, 63), (100, 65), (5, 121), (3000, 131), (17, 249),
+                                   (16, 250), (33, 255), (700, 387), (65, 1021), (4000, 1659), (6, 2041), (13, 2045),
+                                   (300, 2500), (11, 4088), (9, 4089), (10, 4095), (21, 5095), (5, 8184), (4, 8187)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 3), (8, 7)])
+def test_layer_norm_rows_that_start_alike(ops, shape, dtype, pad, offset):
+    """Matrices of one width, pitch and distance from an aligned address, as contiguous ones have."""
+    from paper_2608_15438_gb300 import neuroute as nr
+
+    m, n = shape
+    g = gen(n + pad)
+    x, dy, dres, out, dx = (rows(g, m, n, dtype, pad=pad, offset=offset) for _ in range(5))
+    # what lies around the rows is not theirs, and stays
+    around = []
+    for t in (x, dy, dres, out, dx):
+        whole = t.as_strided((t.untyped_storage().nbytes() // t.element_size(),), (1,), 0)
+        kept = t.clone()
+        whole.fill_(float("nan"))
+        t.copy_(kept)
+        around.append((whole, torch.isnan(whole)))
+    w, b = 1 + 0.3 * torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    u, x64 = U[dtype], x.double()
+    mean64, rstd64 = x64.mean(1), (x64.var(1, unbiased=False) + 1e-5).rsqrt()
+    xh = (x64 - mean64[:, None]) * rstd64[:, None]
+    t = norm_tol(x64, n)
+    ld, dt, f32 = n + pad, ops._DT[dtype], ops._DT[F32]
+    mean, rstd = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    packed = ops._NORM.pack(m, n, dt, f32, 1e-5, x.data_ptr(), ld, 0, w.data_ptr(), b.data_ptr(), out.data_ptr(), ld,
+                            mean.data_ptr(), rstd.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0)
+    assert nr.lib().nr_layer_norm_forward(packed, 0, ops._stream(0)) == 0
+    y64 = xh * w.double() + b.double()
+    near(out, y64, u * y64.abs() + t * (1 + xh.abs()) * w.double().abs() + 2.0 ** -22 * b.double().abs() + TINY[dtype], "y")
+    near(mean, mean64, (n + 16) * 2.0 ** -23 * x64.abs().mean(1), "mean")
+    near(rstd, rstd64, rstd64 * t[:, 0], "rstd")
+    for res in (None, dres):
+        dw, db = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        packed = ops._NORM.pack(m, n, dt, f32, 0.0, x.data_ptr(), ld, 0, w.data_ptr(), 0, 0, 0, mean.data_ptr(),
+                                rstd.data_ptr(), dy.data_ptr(), ld, 0 if res is None else res.data_ptr(), ld,
+                                dx.data_ptr(), ld, dw.data_ptr(), db.data_ptr())
+        need = nr.lib().nr_layer_norm_backward_workspace(packed, 0)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        for turn in range(2):
+            before = [v.clone() for v in (dx, dw, db)]
+            assert nr.lib().nr_layer_norm_backward(packed, 0, ws.data_ptr(), need, ops._stream(0)) == 0
+            assert turn == 0 or all(torch.equal(v, k) for v, k in zip((dx, dw, db), before))
+        r = rstd.double()[:, None]
+        xh = (x64 - mean.double()[:, None]) * r
+        gy = dy.double() * w.double()
+        dx64 = r * (gy - gy.mean(1, keepdim=True) - xh * (gy * xh).mean(1, keepdim=True))
+        if res is not None:
+            dx64 = dx64 + res.double()
+        # the bounds of test_layer_norm
+        exh = 2.0 ** -22 * (1 + (x64.abs() + mean.double().abs()[:, None]) * r)
+        sums = (n + 32) * 2.0 ** -23
+        mag = r * (gy.abs() + gy.abs().mean(1, keepdim=True) * (1 + sums / 2.0 ** -20)
+                   + xh.abs() * (gy * xh).abs().mean(1, keepdim=True) * (1 + sums / 2.0 ** -20))
+        lost = r * (exh * (gy * xh).abs().mean(1, keepdim=True) + xh.abs() * (gy.abs() * exh).mean(1, keepdim=True))
+        near(dx, dx64, u * dx64.abs() + 2.0 ** -20 * mag + lost + TINY[dtype], "dx")
+        dw64, db64 = (dy.double() * xh).sum(0), dy.double().sum(0)
+        sw = (dy.double() * xh).abs().sum(0)
+        near(dw, dw64, U[F32] * dw64.abs() + (m + 32) * 2.0 ** -23 * sw + (dy.double().abs() * exh).sum(0) + TINY[F32], "dw")
+        near(db, db64, U[F32] * db64.abs() + (m + 32) * 2.0 ** -23 * dy.double().abs().sum(0) + TINY[F32], "db")
+    for whole, nans in around:
+        assert torch.equal(torch.isnan(whole), nans)
+
+
 def test_layer_norm_gradients_against_differences(ops):
     g = gen(3)
     m, n = 4, 24
