@@ -27,8 +27,15 @@
 // lets copies in flight land, frees its tensor memory and sets the flag that
 // nr_ops_status reports.
 //
+// Measured, bf16: 65536 x 6144 -> 1536 690 to 730 us, 1.7 PFLOP/s (a library's
+// product reaches 1.9); 10000 x 1536 -> 6144 121 us, 155 with GELU and z kept. Bound
+// by shared memory: a stage takes 600 cycles where its MMAs need 512, as copies
+// and operand reads fill its bandwidth.
+//
 // Up to eight rows run on CUDA cores instead (rows_kernel): the weights are
-// read once, which is all the time such a call can take.
+// read once, which is all the time such a call can take. 1536 -> 6144 takes 6.4
+// us for one row and 15.6 for eight, nine on the tensor cores 13.1; 6144 -> 1536
+// 5.1 and 13.8 against 17.6; 512 -> 512 2.6 and 3.6 against 6.9.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
@@ -604,6 +611,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 }
 
 // ------------------------------------------------------------ few rows, on CUDA cores
+// Bound by reading the weights: 19 MB of them in 6.4 us at one row, from L2.
 // A warp holds MR rows against NR columns of C and KS warps share the columns,
 // each a part of t; x's values are converted once for NR weights.
 constexpr int kRowsThreads = 256;
@@ -705,7 +713,7 @@ struct Saved {
 
 // dz = dy act'(z) rounded to T (unless dz is null), and the column sums of the
 // unrounded values over a block's rows -> sums[blockIdx.y] (unless null). Bound
-// by memory: dy and z read, dz written. A block's threads: x over columns, eight
+// by memory: dy and z read, dz written (4096 x 6144 with GELU 24 us, 6.2 TB/s). A block's threads: x over columns, eight
 // each, y over rows; a thread takes four rows at a time (two at other addresses,
 // which take twice the registers), all loads first. VEC: n is a multiple of 8 and dy
 // and z take 16-byte accesses.
