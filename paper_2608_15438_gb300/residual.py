@@ -30,6 +30,36 @@ from .train import lsim_loss
 _DTYPE = torch.bfloat16
 
 
+class _Once(torch.autograd.Function):
+    """v, with a history (`anchor`'s) whose derivative is an error."""
+
+    @staticmethod
+    def forward(ctx, v, anchor):
+        return v.view_as(v)
+
+    @staticmethod
+    def backward(ctx, dv):
+        raise RuntimeError("the operators' backward passes have no derivatives: "
+                           "gradients of gradients are not supported")
+
+
+def _once(backward):
+    """A backward pass without derivatives of its own. Under create_graph its
+    outputs raise when they are differentiated: without a history a penalty on a
+    gradient would vanish silently. (torch's once_differentiable does so only
+    where the incoming gradient has a history itself.)"""
+
+    def run(ctx, *dy):
+        with torch.no_grad():
+            out = backward(ctx, *dy)
+        if not torch.is_grad_enabled():
+            return out
+        anchor = torch.empty(0, requires_grad=True)
+        return tuple(None if v is None else _Once.apply(v, anchor) for v in out)
+
+    return run
+
+
 class _Linear(torch.autograd.Function):
     """x w^T + b with x [m x k] bf16, w fp32; out fp32 or bf16."""
 
@@ -40,6 +70,7 @@ class _Linear(torch.autograd.Function):
         return ops.linear(x, wh, b, out_dtype=out_dtype)
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         x, wh = ctx.saved_tensors
         need = ctx.needs_input_grad
@@ -55,6 +86,7 @@ class _Norm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         return ops.layer_norm_backward(dy.contiguous(), *ctx.saved_tensors)
 
@@ -73,6 +105,7 @@ class _Block(torch.autograd.Function):
         return ops.linear(a, w2h, b2, residual=r)
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         g, b, mean, rstd, w1h, w2h = ctx.saved_tensors
         r, z = ctx.held[:2]

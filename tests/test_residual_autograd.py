@@ -1,0 +1,158 @@
+"""The residual encoder's autograd functions on the CPU, with a plain stand-in
+for the operators: what they do with gradients of gradients. The stand-in takes
+the operators' arguments and refuses what they refuse."""
+import pytest
+import torch
+
+from paper_2608_15438_gb300 import residual
+
+ACTS = {"none": lambda z: z, "relu": torch.relu, "silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu}
+
+
+class Held:
+    """A checkpoint's stand-in: 32 columns share a power of two."""
+
+    def __init__(self, codes, scales, shape, dtype):
+        self.codes, self.scales, self.shape, self.dtype = codes, scales, tuple(shape), dtype
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+class PlainOps:
+    Checkpoint8 = Held
+
+    @staticmethod
+    def _rows(*ts):
+        for t in ts:
+            if t is not None and t.stride(1) != 1:
+                raise ValueError("rows must be contiguous (stride(1) == 1)")
+
+    @staticmethod
+    def checkpoint8(x):
+        m, n = x.shape
+        g = -(-n // 32)
+        v = torch.nn.functional.pad(x.detach().float(), (0, g * 32 - n)).view(m, g, 32)
+        e = torch.floor(torch.log2(v.abs().amax(2).clamp(min=1e-30) / 127.5)) + 1
+        codes = torch.round(v / torch.exp2(e)[:, :, None]).clamp(-127, 127).to(torch.int8).view(m, g * 32)
+        return Held(codes, (e + 133).to(torch.uint8), (m, n), x.dtype)
+
+    @staticmethod
+    def read(c):
+        if not isinstance(c, Held):
+            return c.float()
+        m, n = c.shape
+        step = torch.exp2(c.scales.float() - 133)[:, :, None]
+        return (c.codes.view(m, -1, 32).float() * step).view(m, -1)[:, :n]
+
+    @classmethod
+    def linear(cls, x, w, bias=None, act="none", residual=None, save=None, out_dtype=None):
+        cls._rows(x, w, residual)
+        z = x.float() @ w.float().T + bias.float()
+        y = ACTS[act](z)
+        if residual is not None:
+            y = y + residual.float()
+        y = y.to(out_dtype or x.dtype)
+        z = z.to(x.dtype)
+        return y if save is None else (y, cls.checkpoint8(z) if save == "z8" else z)
+
+    @classmethod
+    def linear_backward(cls, dy, x, w, z=None, act="none", x_act="none", need=(True, True, True)):
+        cls._rows(dy, w)
+        dz = dy.float()
+        if act != "none":
+            with torch.enable_grad():
+                v = cls.read(z).clone().requires_grad_()
+                (s,) = torch.autograd.grad(ACTS[act](v).sum(), v)
+            dz = dz * s
+        xv = ACTS[x_act](cls.read(x))
+        return ((dz @ w.float()).to(w.dtype) if need[0] else None, (dz.T @ xv).to(w.dtype) if need[1] else None,
+                dz.sum(0) if need[2] else None)
+
+    @classmethod
+    def layer_norm(cls, x, weight, bias, eps=1e-5, save=False):
+        v = cls.read(x)
+        mean, rstd = v.mean(1), (v.var(1, unbiased=False) + eps).rsqrt()
+        y = ((v - mean[:, None]) * rstd[:, None] * weight + bias).to(x.dtype)
+        return (y, mean, rstd) if save else y
+
+    @classmethod
+    def layer_norm_backward(cls, dy, x, weight, mean, rstd, residual_grad=None):
+        cls._rows(dy, residual_grad)
+        xh = (cls.read(x) - mean[:, None]) * rstd[:, None]
+        g = dy.float() * weight
+        dx = rstd[:, None] * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
+        if residual_grad is not None:
+            dx = dx + residual_grad.float()
+        return dx.to(dy.dtype), (dy.float() * xh).sum(0), dy.float().sum(0)
+
+    @staticmethod
+    def check(device=0):
+        pass
+
+
+@pytest.fixture(autouse=True)
+def plain(monkeypatch):
+    monkeypatch.setattr(residual, "ops", PlainOps)
+
+
+def encoder(hold8, D=24, width=32, b=6):
+    return residual.ResidualEncoder(D, width, 2, b, hold8=hold8, device="cpu", seed=1)
+
+
+def rows(m, D, seed=0):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return torch.randn(m, D, generator=g)
+
+
+def test_the_stand_in_gives_the_encoders_gradients():
+    """Against autograd through the formulas in 64 bits; a path of a gradient crosses
+    at most ten roundings to 8 significant bits."""
+    model, x = encoder(False), rows(40, 24)
+    p = {n: v.detach().double().clone().requires_grad_() for n, v in model.named_parameters()}
+    r = x.bfloat16().double() @ p["stem.0"].T + p["stem.1"]
+    norm = torch.nn.functional.layer_norm
+    for i in range(2):
+        q = [p[f"blocks.{i}.{j}"] for j in range(6)]
+        r = r + ACTS["gelu"](norm(r, (32,), q[0], q[1]) @ q[2].T + q[3]) @ q[4].T + q[5]
+    want = norm(r, (32,), p["head.0"], p["head.1"]) @ p["head.2"].T + p["head.3"]
+    dl = rows(40, 6, 1)
+    want.backward(dl.double())
+    model(x).backward(dl)
+    for n, v in model.named_parameters():
+        assert float((v.grad.double() - p[n].grad).norm() / p[n].grad.norm()) <= 0.04, n
+
+
+@pytest.mark.parametrize("hold8", [False, True])
+def test_gradients_of_gradients_are_refused(hold8):
+    """The backward passes have no derivatives of their own: a penalty on a
+    gradient says so instead of losing its share."""
+    model = encoder(hold8)
+    x = rows(40, 24).requires_grad_()
+    out = model(x)
+    dx, = torch.autograd.grad(out, x, torch.ones(40, 6), create_graph=True)
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        (out.sum() + (dx * dx).sum()).backward()
+
+
+@pytest.mark.parametrize("part", ["_Linear", "_Norm"])
+def test_gradients_of_gradients_are_refused_by_each_function(part):
+    x = rows(8, 16).bfloat16().requires_grad_()
+    if part == "_Linear":
+        y = residual._Linear.apply(x, torch.nn.Parameter(rows(4, 16, 2)), torch.nn.Parameter(rows(1, 4, 3)[0]), torch.float32)
+    else:
+        y = residual._Norm.apply(x, torch.nn.Parameter(torch.ones(16)), torch.nn.Parameter(torch.zeros(16)))
+    dx, = torch.autograd.grad(y, x, torch.ones_like(y), create_graph=True)
+    assert dx.requires_grad
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        dx.float().pow(2).sum().backward()
+
+
+def test_a_graph_that_is_not_differentiated_again_is_served():
+    model, x = encoder(True), rows(40, 24)
+    dl = rows(40, 6, 1)
+    want = torch.autograd.grad(model(x), model.stem[0], dl)[0]
+    got = torch.autograd.grad(model(x), model.stem[0], dl, create_graph=True)[0]
+    assert torch.equal(got, want)
