@@ -99,21 +99,29 @@ class _Block(torch.autograd.Function):
         w1h, w2h = w1.to(_DTYPE), w2.to(_DTYPE)
         h, mean, rstd = ops.layer_norm(r, g, b, save=True)
         a, z = ops.linear(h, w1h, b1, act=act, save="z8" if hold8 else "z")
-        ctx.act = act
-        ctx.held = (ops.checkpoint8(r), z) if hold8 else (r, z, h, a)
-        ctx.save_for_backward(g, b, mean, rstd, w1h, w2h)
+        ctx.act, ctx.hold8 = act, hold8
+        # all of it through autograd, which frees it with the block's backward pass, notices
+        # changes in place and offers it to saved-tensor hooks
+        if hold8:
+            r8 = ops.checkpoint8(r)
+            held = (r8.codes, r8.scales, z.codes, z.scales)
+        else:
+            held = (r, z, h, a)
+        ctx.save_for_backward(g, b, mean, rstd, w1h, w2h, *held)
         return ops.linear(a, w2h, b2, residual=r)
 
     @staticmethod
     @_once
     def backward(ctx, dy):
-        g, b, mean, rstd, w1h, w2h = ctx.saved_tensors
-        r, z = ctx.held[:2]
-        if len(ctx.held) == 2:
+        g, b, mean, rstd, w1h, w2h, *held = ctx.saved_tensors
+        if ctx.hold8:
+            m = dy.shape[0]
+            r = ops.Checkpoint8(held[0], held[1], (m, w1h.shape[1]), _DTYPE)
+            z = ops.Checkpoint8(held[2], held[3], (m, w1h.shape[0]), _DTYPE)
             da, dw2, db2 = ops.linear_backward(dy, z, w2h, x_act=ctx.act)
             h = ops.layer_norm(r, g, b)
         else:
-            h, a = ctx.held[2:]
+            r, z, h, a = held
             da, dw2, db2 = ops.linear_backward(dy, a, w2h)
         dh, dw1, db1 = ops.linear_backward(da, h, w1h, z=z, act=ctx.act)
         dr, dg, db = ops.layer_norm_backward(dh, r, g, mean, rstd, residual_grad=dy)

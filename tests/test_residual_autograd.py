@@ -1,6 +1,10 @@
 """The residual encoder's autograd functions on the CPU, with a plain stand-in
-for the operators: what they do with gradients of gradients. The stand-in takes
-the operators' arguments and refuses what they refuse."""
+for the operators: gradients of gradients, and what is kept for the backward
+pass. The stand-in takes the operators' arguments and
+refuses what they refuse."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -156,3 +160,77 @@ def test_a_graph_that_is_not_differentiated_again_is_served():
     want = torch.autograd.grad(model(x), model.stem[0], dl)[0]
     got = torch.autograd.grad(model(x), model.stem[0], dl, create_graph=True)[0]
     assert torch.equal(got, want)
+
+
+def kept(model, x, monkeypatch):
+    """The loss of a step, and weak references to what its forward pass held."""
+    refs = []
+    for name in ("checkpoint8", "linear"):
+        fn = getattr(PlainOps, name)
+
+        def spy(*args, _fn=fn, **kw):
+            out = _fn(*args, **kw)
+            for v in out if isinstance(out, tuple) else (out,):
+                refs.extend(weakref.ref(t) for t in ((v.codes, v.scales) if isinstance(v, Held) else (v,)))
+            return out
+
+        monkeypatch.setattr(PlainOps, name, staticmethod(spy))
+    return model(x).square().mean(), refs
+
+
+@pytest.mark.parametrize("hold8", [False, True])
+def test_a_backward_pass_releases_what_was_held(hold8, monkeypatch):
+    """Also while the loss is still at hand, as in a loop that keeps it for its log."""
+    loss, refs = kept(encoder(hold8), rows(40, 24), monkeypatch)
+    gc.collect()
+    assert sum(r() is not None for r in refs) >= (8 if hold8 else 6)
+    loss.backward()
+    gc.collect()
+    assert [r() for r in refs if r() is not None] == []
+    assert loss.grad_fn is not None
+
+
+@pytest.mark.parametrize("hold8", [False, True])
+def test_hooks_see_all_that_is_held(hold8):
+    """Saved-tensor hooks (offloading, checkpointing) get every activation of a block:
+    the 8-bit codes and scales of its input and pre-activations, or the input,
+    the pre-activations, the norm's output and the activation in 16 bits."""
+    seen = []
+
+    def pack(t):
+        seen.append((t.dtype, tuple(t.shape)))
+        return t.clone()
+
+    model, x = encoder(hold8), rows(40, 24)
+    dl = rows(40, 6, 1)
+    want = torch.autograd.grad(model(x), list(model.parameters()), dl)
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t):
+        out = model(x)
+    got = torch.autograd.grad(out, list(model.parameters()), dl)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    if hold8:
+        for item in ((torch.int8, (40, 32)), (torch.uint8, (40, 1)), (torch.int8, (40, 128)), (torch.uint8, (40, 4))):
+            assert seen.count(item) == 2, item
+    else:
+        assert seen.count((torch.bfloat16, (40, 128))) == 4  # z and a of two blocks
+        assert seen.count((torch.bfloat16, (40, 32))) == 4 + 2  # r and h; the head norm's input and output
+
+
+def test_a_changed_input_of_a_block_is_noticed():
+    p = [v for v in encoder(False).blocks[0]]
+    r = rows(40, 32).bfloat16().requires_grad_()
+    s = r * 1.0
+    y = residual._Block.apply(s, *p, "gelu", False)
+    with torch.no_grad():
+        s.mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward(torch.ones_like(y))
+
+
+def test_a_graph_kept_for_a_second_pass_gives_the_same_gradients():
+    for hold8 in (False, True):
+        model, x = encoder(hold8), rows(40, 24)
+        out, dl = model(x), rows(40, 6, 1)
+        a = torch.autograd.grad(out, list(model.parameters()), dl, retain_graph=True)
+        b = torch.autograd.grad(out, list(model.parameters()), dl)
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
