@@ -60,6 +60,12 @@ def _once(backward):
     return run
 
 
+def _rows(v):
+    """v as the operators take it, its rows contiguous: autograd brings expanded and
+    transposed gradients."""
+    return v if v.stride(1) == 1 else v.contiguous()
+
+
 class _Linear(torch.autograd.Function):
     """x w^T + b with x [m x k] bf16, w fp32; out fp32 or bf16."""
 
@@ -74,7 +80,7 @@ class _Linear(torch.autograd.Function):
     def backward(ctx, dy):
         x, wh = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dw, db = ops.linear_backward(dy, x, wh, need=(need[0], True, True))
+        dx, dw, db = ops.linear_backward(_rows(dy), x, wh, need=(need[0], True, True))
         return dx, dw.float(), db, None
 
 
@@ -88,7 +94,7 @@ class _Norm(torch.autograd.Function):
     @staticmethod
     @_once
     def backward(ctx, dy):
-        return ops.layer_norm_backward(dy.contiguous(), *ctx.saved_tensors)
+        return ops.layer_norm_backward(_rows(dy), *ctx.saved_tensors)
 
 
 class _Block(torch.autograd.Function):
@@ -113,6 +119,7 @@ class _Block(torch.autograd.Function):
     @staticmethod
     @_once
     def backward(ctx, dy):
+        dy = _rows(dy)
         g, b, mean, rstd, w1h, w2h, *held = ctx.saved_tensors
         if ctx.hold8:
             m = dy.shape[0]
@@ -155,7 +162,7 @@ class ResidualEncoder(torch.nn.Module):
 
     def forward(self, x):
         """Logits [m x b] fp32 of scaled rows x [m x D]."""
-        r = _Linear.apply(x.to(_DTYPE), self.stem[0], self.stem[1], _DTYPE)
+        r = _Linear.apply(_rows(x.to(_DTYPE)), self.stem[0], self.stem[1], _DTYPE)
         for p in self.blocks:
             r = _Block.apply(r, p[0], p[1], p[2], p[3], p[4], p[5], self.act, self.hold8)
         return _Linear.apply(_Norm.apply(r, self.head[0], self.head[1]), self.head[2], self.head[3], torch.float32)
@@ -167,7 +174,7 @@ class ResidualEncoder(torch.nn.Module):
         blocks = [(p[0], p[1], p[2].to(_DTYPE), p[3], p[4].to(_DTYPE), p[5]) for p in self.blocks]
         out = []
         for s in range(0, rows.shape[0], batch):
-            r = ops.linear((rows[s:s + batch].float() * in_scale).to(_DTYPE), w[0], self.stem[1])
+            r = ops.linear(_rows((rows[s:s + batch].float() * in_scale).to(_DTYPE)), w[0], self.stem[1])
             for g, b, w1, b1, w2, b2 in blocks:
                 r = ops.linear(ops.linear(ops.layer_norm(r, g, b), w1, b1, act=self.act), w2, b2, residual=r)
             out.append(ops.linear(ops.layer_norm(r, self.head[0], self.head[1]), w[1], self.head[3],

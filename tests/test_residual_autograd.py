@@ -1,6 +1,6 @@
 """The residual encoder's autograd functions on the CPU, with a plain stand-in
-for the operators: gradients of gradients, and what is kept for the backward
-pass. The stand-in takes the operators' arguments and
+for the operators: gradients of gradients, gradients as autograd lays them
+out, and what is kept for the backward pass. The stand-in takes the operators' arguments and
 refuses what they refuse."""
 import gc
 import weakref
@@ -64,7 +64,7 @@ class PlainOps:
     @classmethod
     def linear_backward(cls, dy, x, w, z=None, act="none", x_act="none", need=(True, True, True)):
         cls._rows(dy, w)
-        dz = dy.float()
+        dz = dy.float().contiguous()  # one order of sums for every layout
         if act != "none":
             with torch.enable_grad():
                 v = cls.read(z).clone().requires_grad_()
@@ -89,7 +89,7 @@ class PlainOps:
         dx = rstd[:, None] * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
         if residual_grad is not None:
             dx = dx + residual_grad.float()
-        return dx.to(dy.dtype), (dy.float() * xh).sum(0), dy.float().sum(0)
+        return dx.to(dy.dtype), (dy.float() * xh).sum(0), dy.float().contiguous().sum(0)
 
     @staticmethod
     def check(device=0):
@@ -234,3 +234,43 @@ def test_a_graph_kept_for_a_second_pass_gives_the_same_gradients():
         a = torch.autograd.grad(out, list(model.parameters()), dl, retain_graph=True)
         b = torch.autograd.grad(out, list(model.parameters()), dl)
         assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+LAYOUTS = {"sum": lambda y: y.sum(), "mean": lambda y: y.mean(), "rows": lambda y: y.sum(0).square().sum(),
+           "columns": lambda y: y.sum(1).square().sum(),
+           "transposed": lambda y: (y.T.contiguous() * torch.arange(1.0, y.shape[0] + 1)).sum(),
+           "half": lambda y: y[:, ::2].square().sum()}
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("hold8", [False, True])
+def test_gradients_come_in_any_layout(hold8, layout):
+    """Autograd brings expanded and transposed gradients; they give what contiguous ones give."""
+    model, x = encoder(hold8), rows(40, 24)
+    leaf = model(x).detach().requires_grad_()
+    LAYOUTS[layout](leaf).backward()
+    want = torch.autograd.grad(model(x), list(model.parameters()), leaf.grad.contiguous())
+    got = torch.autograd.grad(LAYOUTS[layout](model(x)), list(model.parameters()))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("layout", ["sum", "transposed"])
+@pytest.mark.parametrize("part", ["linear", "norm", "block8", "block16"])
+def test_each_function_takes_a_gradient_in_any_layout(part, layout):
+    x = rows(8, 32).bfloat16().requires_grad_()
+    g, b = torch.ones(32), torch.zeros(32)
+    if part == "linear":
+        y = residual._Linear.apply(x, rows(12, 32, 2), torch.zeros(12), torch.float32)
+    elif part == "norm":
+        y = residual._Norm.apply(x, g, b)
+    else:
+        y = residual._Block.apply(x, *[v.detach() for v in encoder(False).blocks[0]], "gelu", part == "block8")
+    dy = torch.ones(1, 1, dtype=y.dtype).expand(y.shape) if layout == "sum" else rows(y.shape[1], 8, 4).to(y.dtype).T
+    want, = torch.autograd.grad(y, x, dy.contiguous(), retain_graph=True)
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], want)
+
+
+def test_rows_to_encode_come_in_any_layout():
+    model, x = encoder(True), rows(24, 40).T
+    assert torch.equal(model(x), model(x.contiguous()))
+    assert torch.equal(model.encode(x), model.encode(x.contiguous()))
