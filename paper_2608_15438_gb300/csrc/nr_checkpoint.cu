@@ -95,12 +95,9 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
         for (int q = 0; q < 4; ++q) p[q] = act_value2(p[q], act);
       }
-      if (TypeCode<T>::code == NR_F16 && s[u] >= 143u) {  // 64 x 2^10 stands for up to 65504: keep it finite; NaN stays
+      if (TypeCode<T>::code == NR_F16 && s[u] >= kHeld8F16) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          p[q].x = p[q].x > 65504.0f ? 65504.0f : p[q].x < -65504.0f ? -65504.0f : p[q].x;
-          p[q].y = p[q].y > 65504.0f ? 65504.0f : p[q].y < -65504.0f ? -65504.0f : p[q].y;
-        }
+        for (int q = 0; q < 4; ++q) p[q] = held8_in_f16(p[q]);
       }
       const float v[8] = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
       if (VEC || sizeof(T) == 4) {

@@ -144,7 +144,8 @@ __device__ __forceinline__ void settle_raw(Eight<T> &o, const T *row, int v, int
   settle_eight<T>(o, row + c, false, min(8, n - c), lo, hi);
 }
 // x, which may be a checkpoint: then the codes as numbers of T, exactly, and
-// their scale
+// their scale (in fp16 near the type's end: the values that they stand for, as
+// exact there, and 1)
 template <int TPR, typename T>
 __device__ __forceinline__ Eight<T> load_held(const Rows &x, int64_t i, int v, int t, int n, float &scale, int width = TPR) {
   Eight<T> o = {};
@@ -152,10 +153,16 @@ __device__ __forceinline__ Eight<T> load_held(const Rows &x, int64_t i, int v, i
   const int c = column<TPR>(1, v, 0, t, width);
   if (c < n) {
     const uint2 a = __ldg(reinterpret_cast<const uint2 *>(static_cast<const int8_t *>(x.p) + i * x.groups * kOpsGroup + c));
-    scale = held8_down(__ldg(x.scale + i * x.groups + (c >> 5)));
+    const uint32_t s = __ldg(x.scale + i * x.groups + (c >> 5));
+    scale = held8_down(s);
     float2 p[4];
     held8_numbers(a.x, p[0], p[1]);
     held8_numbers(a.y, p[2], p[3]);
+    if (TypeCode<T>::code == NR_F16 && s >= kHeld8F16) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) p[q] = held8_in_f16(mul2(p[q], both(scale)));
+      scale = 1.0f;
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (sizeof(T) == 4) {
@@ -725,8 +732,9 @@ constexpr int kLong = 16384, kLongThreads = 512;
 
 __device__ __forceinline__ float long_x(const Rows &x, int64_t i, int64_t j, int dtype) {
   if (!x.scale) return load_any(x.p, i * x.ld + j, dtype);
-  return (float)static_cast<const int8_t *>(x.p)[i * x.groups * kOpsGroup + j] *
-         held8_down(x.scale[i * x.groups + (j >> 5)]);
+  const float v = (float)static_cast<const int8_t *>(x.p)[i * x.groups * kOpsGroup + j] *
+                  held8_down(x.scale[i * x.groups + (j >> 5)]);
+  return dtype == NR_F16 ? held8_in_f16(make_float2(v, v)).x : v;
 }
 
 __global__ void __launch_bounds__(kLongThreads) long_forward_kernel(const Norm N, int dtype) {

@@ -324,6 +324,13 @@ __device__ __forceinline__ float held8_up(uint32_t s) {
 __device__ __forceinline__ float held8_down(uint32_t s) {
   return s == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float((s - 6u) << 23);
 }
+// What a held number stands for in fp16, where 64 x 2^10 is past the type's end:
+// at most the largest finite value. From scale kHeld8F16 (2^10) on; NaN stays.
+constexpr uint32_t kHeld8F16 = 143u;
+__device__ __forceinline__ float2 held8_in_f16(float2 v) {
+  return make_float2(v.x > 65504.0f ? 65504.0f : v.x < -65504.0f ? -65504.0f : v.x,
+                     v.y > 65504.0f ? 65504.0f : v.y < -65504.0f ? -65504.0f : v.y);
+}
 // The codes of four values in a word. Adding 1.5 2^23 rounds to a whole number,
 // ties to even, and leaves its two's complement in the low byte (a conversion
 // instruction runs at half the rate or less). Only the topmost scale (and 255)
