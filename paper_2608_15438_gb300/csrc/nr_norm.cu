@@ -22,6 +22,7 @@
 // Measured (a copy reaches 6.8 TB/s), bf16: forward 262144 x 1536 292 us, 5.5 TB/s;
 // backward 455 us, 5.3 TB/s, with a residual's gradient 592 us, 5.4 TB/s.
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "nrq_ops.cuh"
@@ -824,7 +825,8 @@ Norm norm_of(const nr_layer_norm *a, bool backward) {
   N.weight = a->weight;
   N.bias = a->bias;
   N.w_dtype = (int)a->w_dtype;
-  N.eps = (float)a->eps;
+  // at least the least fp32: an eps below it is positive too (a row without deviation times infinity was NaN)
+  N.eps = fmaxf((float)a->eps, 1.40129846e-45f);
   N.y = a->y;
   N.y_ld = a->y_ld;
   N.mean = a->mean;
