@@ -96,8 +96,8 @@ typedef struct {
   void *dbias;         /* [n]; backward: out, or NULL */
 } nr_linear;
 
-/* Scratch bytes of a call with these sizes, types, alignments and outputs; a
- * negative value if the arguments are invalid. */
+/* Scratch bytes of a call with these sizes, types, alignments and outputs, or
+ * NR_ERR_INVALID_ARG, or NR_ERR_CUDA if the device is not there (both negative). */
 int64_t nr_linear_forward_workspace(const nr_linear *a, int device);
 int64_t nr_linear_backward_workspace(const nr_linear *a, int device);
 
@@ -129,6 +129,7 @@ typedef struct {
   void *dweight, *dbias; /* [n]; backward: out, or both NULL */
 } nr_layer_norm;
 
+/* as nr_linear_backward_workspace */
 int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int device);
 nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, void *stream);
 nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, void *ws, int64_t ws_bytes,

@@ -132,11 +132,12 @@ extern "C" nr_status nr_checkpoint8_write(const void *x, int dtype, int64_t m, i
                                           void *scales, int device, void *stream) {
   if (!valid(codes, scales, x, m, n, dtype) || x_ld < 0) return NR_ERR_INVALID_ARG;
   if (m == 0) return NR_OK;
+  const int sms = nr_ops_sms(device);
   DeviceGuard g(device);
-  if (!g.ok) return NR_ERR_CUDA;
+  if (sms < 1 || !g.ok) return NR_ERR_CUDA;
   const int64_t groups = ceil_div(n, kOpsGroup);
   dim3 grid, block;
-  cut(m, n, nr_ops_sms(device), grid, block);
+  cut(m, n, sms, grid, block);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool vec = n % 8 == 0 && vec_ok(x, x_ld, dtype);
   int8_t *c = static_cast<int8_t *>(codes);
@@ -160,11 +161,12 @@ extern "C" nr_status nr_checkpoint8_read(const void *codes, const void *scales, 
                                          int dtype, int64_t y_ld, int device, void *stream) {
   if (!valid(codes, scales, y, m, n, dtype) || !act_ok(act) || y_ld < n) return NR_ERR_INVALID_ARG;
   if (m == 0) return NR_OK;
+  const int sms = nr_ops_sms(device);
   DeviceGuard g(device);
-  if (!g.ok) return NR_ERR_CUDA;
+  if (sms < 1 || !g.ok) return NR_ERR_CUDA;
   const int64_t groups = ceil_div(n, kOpsGroup);
   dim3 grid, block;
-  cut(m, n, nr_ops_sms(device), grid, block);
+  cut(m, n, sms, grid, block);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool vec = n % 8 == 0 && vec_ok(y, y_ld, dtype);
   const int8_t *c = static_cast<const int8_t *>(codes);
@@ -192,12 +194,12 @@ __device__ int ops_flag;
 
 int nr_ops_sms(int device) {
   static int sms[kOpsDevices];  // 0: not looked up yet; a race writes the same value
-  if (device < 0 || device >= kOpsDevices) return 1;
+  if (device < 0 || device >= kOpsDevices) return 0;
   if (sms[device] == 0) {
     int v = 0;
     if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || v < 1) {
       cudaGetLastError();
-      return 1;
+      return 0;
     }
     sms[device] = v;
   }

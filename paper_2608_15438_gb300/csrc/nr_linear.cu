@@ -888,6 +888,7 @@ Cut choose(int64_t rows, int64_t n, int64_t slices, bool b_outer, int cg_only, i
   for (int cg = 1; cg <= 2; ++cg) {
     if (cg_only ? cg != cg_only : cg == 2 && rows <= kRows) continue;
     const int64_t tm = ceil_div(rows, (int64_t)kRows * cg), slot = sms / cg;
+    if (slot < 1) continue;
     for (int nt = 32; nt <= 256; nt *= 2) {
       if (cg == 2 && nt < 128) continue;
       if (b_outer && nt / cg < 64) continue;
@@ -1059,7 +1060,7 @@ struct ForwardPlan {
   int64_t x_at = -1, w_at = -1, parts_at = -1, z_at = -1, bytes = 0;
   Cut cut = {1, 32, 1};
 };
-ForwardPlan plan_forward(const nr_linear *a, int device) {
+ForwardPlan plan_forward(const nr_linear *a, int sms) {
   ForwardPlan f;
   f.few = a->m <= kFewRows;
   f.x = {a->x, a->x_ld, a->m, a->k, false};
@@ -1072,7 +1073,7 @@ ForwardPlan plan_forward(const nr_linear *a, int device) {
   }
   if (!mappable(f.x)) f.x_at = s.take(a->m * round_up(a->k, 8) * 2);
   if (!mappable(f.w)) f.w_at = s.take(a->n * round_up(a->k, 8) * 2);
-  f.cut = choose(a->m, a->n, ceil_div(a->k, kSlice), false, 0, nr_ops_sms(device));
+  f.cut = choose(a->m, a->n, ceil_div(a->k, kSlice), false, 0, sms);
   if (f.cut.splits > 1) f.parts_at = s.take(parts_bytes(f.cut, a->m, a->n));
   f.bytes = s.at;
   return f;
@@ -1130,10 +1131,9 @@ struct BackwardPlan {
   int64_t dz_at = -1, x_at = -1, w_at = -1, sums_at = -1, dx_at = -1, dw_at = -1, bytes = 0;
   Cut dx = {1, 64, 1}, dw = {1, 64, 1};
 };
-BackwardPlan plan_backward(const nr_linear *a, int device) {
+BackwardPlan plan_backward(const nr_linear *a, int sms) {
   BackwardPlan b;
   Scratch s;
-  const int sms = nr_ops_sms(device);
   const int64_t m = a->m, n = a->n, k = a->k;
   b.dz = {a->dy, a->dy_ld, m, n, false};
   b.x = {a->x, a->x_ld, m, k, true};
@@ -1189,13 +1189,17 @@ void *at(void *ws, int64_t o) { return o < 0 ? nullptr : static_cast<char *>(ws)
 }  // namespace
 
 extern "C" int64_t nr_linear_forward_workspace(const nr_linear *a, int device) {
-  return valid(a, false) ? plan_forward(a, device).bytes : -1;
+  if (!valid(a, false)) return NR_ERR_INVALID_ARG;
+  const int sms = nr_ops_sms(device);
+  return sms > 0 ? plan_forward(a, sms).bytes : (int64_t)NR_ERR_CUDA;
 }
 
 extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws, int64_t ws_bytes, void *stream) {
   if (!valid(a, false)) return NR_ERR_INVALID_ARG;
   if (a->m == 0) return NR_OK;
-  ForwardPlan f = plan_forward(a, device);
+  const int sms = nr_ops_sms(device);
+  if (sms < 1) return NR_ERR_CUDA;
+  ForwardPlan f = plan_forward(a, sms);
   if (ws_bytes < f.bytes || (f.bytes > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)))) return NR_ERR_INVALID_ARG;
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;
@@ -1224,8 +1228,8 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
       E.z = at(ws, f.z_at);
       E.z_ld = a->n;
     }
-    if (a->dtype == NR_F16) launch_rows_any<__half>(a, E, nr_ops_sms(device), s);
-    else launch_rows_any<__nv_bfloat16>(a, E, nr_ops_sms(device), s);
+    if (a->dtype == NR_F16) launch_rows_any<__half>(a, E, sms, s);
+    else launch_rows_any<__nv_bfloat16>(a, E, sms, s);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_status(e);
     return a->z_scale ? nr_checkpoint8_write(E.z, NR_F32, a->m, a->n, a->n, a->z, a->z_scale, device, stream) : NR_OK;
@@ -1247,12 +1251,16 @@ extern "C" nr_status nr_linear_forward(const nr_linear *a, int device, void *ws,
 }
 
 extern "C" int64_t nr_linear_backward_workspace(const nr_linear *a, int device) {
-  return valid(a, true) ? plan_backward(a, device).bytes : -1;
+  if (!valid(a, true)) return NR_ERR_INVALID_ARG;
+  const int sms = nr_ops_sms(device);
+  return sms > 0 ? plan_backward(a, sms).bytes : (int64_t)NR_ERR_CUDA;
 }
 
 extern "C" nr_status nr_linear_backward(const nr_linear *a, int device, void *ws, int64_t ws_bytes, void *stream) {
   if (!valid(a, true)) return NR_ERR_INVALID_ARG;
-  BackwardPlan b = plan_backward(a, device);
+  const int sms = nr_ops_sms(device);
+  if (sms < 1) return NR_ERR_CUDA;
+  BackwardPlan b = plan_backward(a, sms);
   if (ws_bytes < b.bytes || (b.bytes > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)))) return NR_ERR_INVALID_ARG;
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;

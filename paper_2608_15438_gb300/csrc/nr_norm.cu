@@ -961,14 +961,15 @@ constexpr int kLongParts = 32;
 extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, void *stream) {
   if (!valid(a, false)) return NR_ERR_INVALID_ARG;
   if (a->m == 0) return NR_OK;
+  const int sms = nr_ops_sms(device);
   DeviceGuard g(device);
-  if (!g.ok) return NR_ERR_CUDA;
+  if (sms < 1 || !g.ok) return NR_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Norm N = norm_of(a, false);
   const Shape sh = shape_of(N, a->dtype != NR_F32, false);
   cudaError_t e;
   if (sh.threads) {
-    e = launch_any(N, sh, false, a->dtype, block_count(sh, N, a->dtype != NR_F32, false, nr_ops_sms(device)), s);
+    e = launch_any(N, sh, false, a->dtype, block_count(sh, N, a->dtype != NR_F32, false, sms), s);
   } else {
     long_forward_kernel<<<(unsigned)a->m, kLongThreads, 0, s>>>(N, (int)a->dtype);
     e = cudaGetLastError();
@@ -977,17 +978,20 @@ extern "C" nr_status nr_layer_norm_forward(const nr_layer_norm *a, int device, v
 }
 
 extern "C" int64_t nr_layer_norm_backward_workspace(const nr_layer_norm *a, int device) {
-  if (!valid(a, true)) return -1;
+  if (!valid(a, true)) return NR_ERR_INVALID_ARG;
+  const int sms = nr_ops_sms(device);
+  if (sms < 1) return NR_ERR_CUDA;
   if (a->m == 0 || !a->dweight) return 0;
   const Norm N = norm_of(a, true);
   const Shape sh = shape_of(N, a->dtype != NR_F32, true);
-  const int64_t blocks = sh.threads ? block_count(sh, N, a->dtype != NR_F32, true, nr_ops_sms(device)) : kLongParts;
+  const int64_t blocks = sh.threads ? block_count(sh, N, a->dtype != NR_F32, true, sms) : kLongParts;
   return round_up(blocks * 2 * a->n * 4, 256);
 }
 
 extern "C" nr_status nr_layer_norm_backward(const nr_layer_norm *a, int device, void *ws, int64_t ws_bytes, void *stream) {
   const int64_t need = nr_layer_norm_backward_workspace(a, device);
-  if (need < 0 || ws_bytes < need || (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))))
+  if (need < 0) return (nr_status)need;
+  if (ws_bytes < need || (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))))
     return NR_ERR_INVALID_ARG;
   DeviceGuard g(device);
   if (!g.ok) return NR_ERR_CUDA;

@@ -368,7 +368,7 @@ inline bool vec_ok(const void *p, int64_t ld, int64_t dtype) {
 inline bool act_ok(int64_t a) { return a >= NR_ACT_NONE && a <= NR_ACT_SILU; }
 constexpr int64_t kOpsMaxRows = ((int64_t)1 << 31) - 1, kOpsMaxCols = ((int64_t)1 << 24) - 1;
 
-// the SM count of a device, looked up once
+// the SM count of a device, looked up once; 0: there is no such device
 int nr_ops_sms(int device);
 // the device's flag that expired waits set (the address, looked up once)
 cudaError_t nr_ops_flag(int device, int **flag);

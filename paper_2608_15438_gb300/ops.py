@@ -146,7 +146,7 @@ def _scratch(call, nbytes, device):
     """Scratch of a call and its address."""
     if nbytes <= 0:
         if nbytes < 0:
-            raise _nr.NRError(call, -1)
+            raise _nr.NRError(call, nbytes)
         return None, 0
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return ws, ws.data_ptr()
