@@ -101,8 +101,9 @@ typedef struct {
 int64_t nr_linear_forward_workspace(const nr_linear *a, int device);
 int64_t nr_linear_backward_workspace(const nr_linear *a, int device);
 
-/* Errors: NR_ERR_INVALID_ARG (sizes, types, a missing pointer, ws_bytes too
- * small), NR_ERR_CUDA. */
+/* Errors: NR_ERR_INVALID_ARG (sizes, types, a missing pointer, a matrix or codes
+ * at an address that is no multiple of their alignment, ws_bytes too small),
+ * NR_ERR_CUDA. */
 nr_status nr_linear_forward(const nr_linear *a, int device, void *ws, int64_t ws_bytes, void *stream);
 nr_status nr_linear_backward(const nr_linear *a, int device, void *ws, int64_t ws_bytes, void *stream);
 

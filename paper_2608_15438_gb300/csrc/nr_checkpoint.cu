@@ -123,7 +123,7 @@ void cut(int64_t m, int64_t n, int sms, dim3 &grid, dim3 &block) {
 
 bool valid(const void *codes, const void *scales, const void *v, int64_t m, int64_t n, int dtype) {
   if (m < 0 || m > kOpsMaxRows || n < 1 || n > kOpsMaxCols || dtype < NR_F32 || dtype > NR_BF16) return false;
-  return m == 0 || (codes && scales && v && (reinterpret_cast<uintptr_t>(codes) & 15) == 0);
+  return m == 0 || (codes && scales && v && placed(codes, dtype, true) && placed(v, dtype));
 }
 
 }  // namespace

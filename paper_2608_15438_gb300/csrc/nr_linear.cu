@@ -1030,14 +1030,20 @@ bool valid(const nr_linear *a, bool backward) {
       (a->bias_dtype != a->dtype && a->bias_dtype != NR_F32) || !act_ok(a->act) || !act_ok(a->x_act))
     return false;
   if (a->x_ld < 0 || a->w_ld < 0 || a->residual_ld < 0 || a->dy_ld < 0) return false;
-  if (a->m > 0 && (!a->x || !a->w)) return false;
+  if (a->m > 0 && (!a->x || !a->w || !placed(a->x, a->dtype, a->x_scale) || !placed(a->w, a->dtype))) return false;
   if (!backward) {
     if (a->x_scale || a->x_act) return false;
     if (a->m > 0 && (!a->y || a->y_ld < a->n || (a->z && !a->z_scale && a->z_ld < a->n))) return false;
+    if (a->m > 0 && (!placed(a->y, a->y_dtype) || !placed(a->z, a->dtype, a->z_scale) || !placed(a->residual, a->dtype) ||
+                     !placed(a->bias, a->bias_dtype)))
+      return false;
     return !(a->z_scale && !a->z);
   }
   if (a->x_act && !a->x_scale) return false;
   if (a->m > 0 && (!a->dy || (a->act != NR_ACT_NONE && !a->z))) return false;
+  if (a->m > 0 && (!placed(a->dy, a->y_dtype) || (a->act != NR_ACT_NONE && !placed(a->z, a->dtype, a->z_scale)) ||
+                   !placed(a->dx, a->dtype) || !placed(a->dw, a->dtype) || !placed(a->dbias, a->bias_dtype)))
+    return false;
   return !(a->m > 0 && a->dx && a->dx_ld < a->k);
 }
 

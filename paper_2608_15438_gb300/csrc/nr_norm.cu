@@ -811,6 +811,13 @@ bool valid(const nr_layer_norm *a, bool backward) {
   if (!a || a->m < 0 || a->m > kOpsMaxRows || a->n < 1 || a->n > kOpsMaxCols) return false;
   if (a->dtype < NR_F32 || a->dtype > NR_BF16 || (a->w_dtype != a->dtype && a->w_dtype != NR_F32)) return false;
   if (a->x_ld < 0 || a->dy_ld < 0 || a->residual_grad_ld < 0 || (a->m > 0 && !a->x)) return false;
+  if (a->m > 0 && (!placed(a->x, a->dtype, a->x_scale) || !placed(a->weight, a->w_dtype) || !placed(a->mean, NR_F32) ||
+                   !placed(a->rstd, NR_F32)))
+    return false;
+  if (a->m > 0 && (backward ? !placed(a->dy, a->dtype) || !placed(a->residual_grad, a->dtype) || !placed(a->dx, a->dtype) ||
+                                  !placed(a->dweight, a->w_dtype) || !placed(a->dbias, a->w_dtype)
+                            : !placed(a->bias, a->w_dtype) || !placed(a->y, a->dtype)))
+    return false;
   if (!backward)
     return a->eps > 0.0 && !a->mean == !a->rstd && (a->m == 0 || (a->y && a->y_ld >= a->n));
   return !a->dweight == !a->dbias &&

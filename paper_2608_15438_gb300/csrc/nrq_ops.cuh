@@ -365,6 +365,10 @@ inline size_t type_bytes(int64_t t) { return t == NR_F32 ? 4 : 2; }
 inline bool vec_ok(const void *p, int64_t ld, int64_t dtype) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (int64_t)type_bytes(dtype) % 16 == 0;
 }
+// whether a matrix (values of a type, or a checkpoint's codes) lies where the kernels' accesses can reach it
+inline bool placed(const void *p, int64_t dtype, bool codes = false) {
+  return (reinterpret_cast<uintptr_t>(p) & (codes ? 15 : type_bytes(dtype) - 1)) == 0;
+}
 inline bool act_ok(int64_t a) { return a >= NR_ACT_NONE && a <= NR_ACT_SILU; }
 constexpr int64_t kOpsMaxRows = ((int64_t)1 << 31) - 1, kOpsMaxCols = ((int64_t)1 << 24) - 1;
 
