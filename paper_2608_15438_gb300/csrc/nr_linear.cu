@@ -1041,6 +1041,7 @@ bool valid(const nr_linear *a, bool backward) {
   }
   if (a->x_act && !a->x_scale) return false;
   if (a->m > 0 && (!a->dy || (a->act != NR_ACT_NONE && !a->z))) return false;
+  if (a->act != NR_ACT_NONE && !a->z_scale && a->z_ld < 0) return false;
   if (a->m > 0 && (!placed(a->dy, a->y_dtype) || (a->act != NR_ACT_NONE && !placed(a->z, a->dtype, a->z_scale)) ||
                    !placed(a->dx, a->dtype) || !placed(a->dw, a->dtype) || !placed(a->dbias, a->bias_dtype)))
     return false;

@@ -1,5 +1,6 @@
-"""The C entries' refusals of addresses: codes must lie at 16-byte addresses
-wherever a call takes them, other values at multiples of their size."""
+"""The C entries' refusals of addresses and pitches: codes must lie at 16-byte
+addresses wherever a call takes them, other values at multiples of their size,
+and no pitch may be negative."""
 import pytest
 
 from paper_2608_15438_gb300 import neuroute as nr
@@ -64,6 +65,17 @@ def test_values_between_their_types_addresses_are_refused():
     for dtype, off in ((0, 2), (1, 1), (2, 1)):
         assert L.nr_checkpoint8_write(P + off, dtype, 4, 32, 32, P, P, 0, None) == INVALID
         assert L.nr_checkpoint8_read(P, P, 4, 32, 0, P + off, dtype, 32, 0, None) == INVALID
+
+
+def test_negative_pitches_are_refused():
+    L = nr.lib()
+    for kw in (dict(z=P, z_ld=-8), dict(z=P, z_ld=96, x_ld=-1), dict(z=P, z_ld=96, w_ld=-1), dict(z=P, z_ld=96, dy_ld=-96)):
+        assert L.nr_linear_backward_workspace(lin(**kw), 0) == INVALID, kw
+        assert L.nr_linear_backward(lin(**kw), 0, P, 1 << 40, None) == INVALID, kw
+    for kw in (dict(x_scale=0, x_ld=-1), dict(dy_ld=-1), dict(rg=P, rg_ld=-1), dict(dx_ld=-96)):
+        assert L.nr_layer_norm_backward_workspace(norm(**kw), 0) == INVALID, kw
+    assert L.nr_layer_norm_forward(norm(x_scale=0, x_ld=-1), 0, None) == INVALID
+    assert L.nr_checkpoint8_write(P, 2, 4, 32, -1, P, P, 0, None) == INVALID
 
 
 def test_empty_batches_need_no_addresses():
