@@ -150,8 +150,9 @@ nr_status nr_checkpoint8_read(const void *codes, const void *scales, int64_t m, 
 nr_status nr_ops_status(int device);
 
 /* Execution only: the limit of the bounded waits, in microseconds, for calls
- * that follow. 0 (default): 1 s. < 0: a wait whose phase is not complete when
- * first tested expires at once, which exercises the failure path. */
+ * that follow, at most 60000000 (else NR_ERR_INVALID_ARG and no change). 0
+ * (default): 1 s. < 0: a wait whose phase is not complete when first tested
+ * expires at once, which exercises the failure path. */
 nr_status nr_ops_wait_limit(int64_t us);
 
 #ifdef __cplusplus

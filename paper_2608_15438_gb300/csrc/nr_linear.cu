@@ -1340,6 +1340,7 @@ extern "C" nr_status nr_linear_backward(const nr_linear *a, int device, void *ws
 }
 
 extern "C" nr_status nr_ops_wait_limit(int64_t us) {
+  if (us > 60000000) return NR_ERR_INVALID_ARG;
   wait_limit = us == 0 ? kWaitNs : us < 0 ? (int64_t)-1 : us * 1000;
   return NR_OK;
 }
