@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "nrq_ops.cuh"
 
 namespace {
@@ -193,7 +195,7 @@ __device__ int ops_flag;
 }  // namespace
 
 int nr_ops_sms(int device) {
-  static int sms[kOpsDevices];  // 0: not looked up yet; a race writes the same value
+  static std::atomic<int> sms[kOpsDevices];  // 0: not looked up yet; threads that race write the same value
   if (device < 0 || device >= kOpsDevices) return 0;
   if (sms[device] == 0) {
     int v = 0;
@@ -207,7 +209,7 @@ int nr_ops_sms(int device) {
 }
 
 cudaError_t nr_ops_flag(int device, int **flag) {
-  static int *flags[kOpsDevices];
+  static std::atomic<int *> flags[kOpsDevices];
   if (device < 0 || device >= kOpsDevices) return cudaErrorInvalidDevice;
   if (!flags[device]) {
     void *p = nullptr;

@@ -42,6 +42,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "nrq_ops.cuh"
 #include "nrq_tc.cuh"
 
@@ -915,7 +917,7 @@ int64_t parts_bytes(const Cut &c, int64_t rows, int64_t n) {
   return c.splits > 1 ? round_up(c.splits * rows * round_up(n, 8) * 4, 256) : 0;
 }
 
-int64_t wait_limit = kWaitNs;  // nr_ops_wait_limit
+std::atomic<int64_t> wait_limit{kWaitNs};  // nr_ops_wait_limit, from any thread
 
 // an operand pair, its cut and what becomes of C
 struct Task {
@@ -929,7 +931,7 @@ struct Task {
 template <int CG>
 cudaError_t launch_product(const CUtensorMap (&m)[4], const Job &J, uint32_t smem, int grid, int device, bool follows,
                            cudaStream_t s) {
-  static bool ready[64];  // the attribute is set once a device
+  static std::atomic<bool> ready[64];  // the attribute is set once a device (twice by threads that race)
   if (!ready[device]) {
     const cudaError_t e =
         cudaFuncSetAttribute(product_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);

@@ -28,3 +28,50 @@ def test_an_eps_below_fp32s_range_is_still_positive(ops, n, dtype):
         y, mean, rstd = ops.layer_norm(x, None, b, eps=eps, save=True)
         assert torch.equal(y, b.expand(3, n)), eps
         assert torch.equal(mean, x[:, 0].float()) and rstd.isfinite().all()
+
+
+def test_calls_from_several_threads(ops):
+    """Each on a stream of its own, while another thread sets the waits' limit to what it is."""
+    import threading
+
+    from paper_2608_15438_gb300 import neuroute as nr
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    x = torch.randn(600, 256, generator=g, device="cuda").to(BF16)
+    w = (torch.randn(512, 256, generator=g, device="cuda") / 16).to(BF16)
+    dy = torch.randn(600, 512, generator=g, device="cuda").to(BF16)
+
+    def step():
+        h = ops.layer_norm(x)
+        y, z = ops.linear(h, w, act="gelu", save="z8")
+        return (y,) + ops.linear_backward(dy, h, w, z=z, act="gelu")
+
+    want = step()
+    torch.cuda.synchronize()
+    wrong, done = [], threading.Event()
+
+    def work():
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = step()
+                s.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    wrong.append(1)
+
+    def limits():
+        while not done.is_set():
+            assert nr.lib().nr_ops_wait_limit(0) == 0
+
+    threads = [threading.Thread(target=work) for _ in range(6)]
+    other = threading.Thread(target=limits)
+    other.start()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    done.set()
+    other.join()
+    assert not wrong
+    ops.check(0)
