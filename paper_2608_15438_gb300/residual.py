@@ -168,8 +168,10 @@ class ResidualEncoder(torch.nn.Module):
         return _Linear.apply(_Norm.apply(r, self.head[0], self.head[1]), self.head[2], self.head[3], torch.float32)
 
     @torch.no_grad()
-    def encode(self, rows, in_scale: float = 1.0, batch: int = 1 << 17):
-        """Logits of rows [n x D] (uint8 or fp32), `batch` rows at a time."""
+    def encode(self, rows, in_scale: float = 1.0, batch: int = 1 << 17, check: bool = True):
+        """Logits of rows [n x D] (uint8 or fp32), `batch` rows at a time. check: waits
+        for them and raises if a bounded wait expired on their way (ops.check); without it, and
+        while a CUDA graph is captured, that is the caller's to do before the logits are used."""
         w = [p.to(_DTYPE) for p in (self.stem[0], self.head[2])]
         blocks = [(p[0], p[1], p[2].to(_DTYPE), p[3], p[4].to(_DTYPE), p[5]) for p in self.blocks]
         out = []
@@ -179,7 +181,10 @@ class ResidualEncoder(torch.nn.Module):
                 r = ops.linear(ops.linear(ops.layer_norm(r, g, b), w1, b1, act=self.act), w2, b2, residual=r)
             out.append(ops.linear(ops.layer_norm(r, self.head[0], self.head[1]), w[1], self.head[3],
                                   out_dtype=torch.float32))
-        return torch.cat(out) if len(out) != 1 else out[0]
+        out = torch.cat(out) if len(out) != 1 else out[0]
+        if check and out.is_cuda and not torch.cuda.is_current_stream_capturing():
+            ops.check(out.device)
+        return out
 
 
 def train_residual(x, in_scale: float, width: int, blocks: int, b: int, epochs: int = 100, batch: int = 4096,
@@ -187,7 +192,8 @@ def train_residual(x, in_scale: float, width: int, blocks: int, b: int, epochs: 
                    log=None):
     """Train on the rows x [n x D] (a device tensor, uint8 or fp32) with L_sim as
     train.train_encoder does; returns (encoder, history), history one (epoch,
-    mean loss, mean tau_emb, seconds) per epoch."""
+    mean loss, mean tau_emb, seconds) per epoch. Raises after an epoch in which a
+    bounded wait expired."""
     model = ResidualEncoder(x.shape[1], width, blocks, b, hold8=hold8, device=x.device, seed=seed)
     opt = torch.optim.Adam(model.parameters(), lr=lr)
     g = torch.Generator(device=x.device)
@@ -205,6 +211,7 @@ def train_residual(x, in_scale: float, width: int, blocks: int, b: int, epochs: 
             tot += loss.detach()
             ttot += tau
             nb += 1
+        ops.check(x.device)  # outputs after an expired wait are undefined: no further epoch on them
         hist.append((ep, float(tot) / max(nb, 1), float(ttot) / max(nb, 1), time.time() - t0))
         if log is not None:
             log(hist[-1])
