@@ -381,5 +381,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual_grad=None, param_gra
 def check(device=0):
     """Waits for the device and raises if a bounded wait inside one of these
     operators' kernels expired since the last check (nr_ops_status)."""
-    _nr._check("nr_ops_status", _nr.lib().nr_ops_status(torch.device("cuda", device).index
-                                                         if isinstance(device, int) else device.index))
+    d = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+    if d.type != "cuda":
+        raise ValueError(f"device: {device}, expected a CUDA device")
+    index = torch.cuda.current_device() if d.index is None else d.index
+    _nr._check("nr_ops_status", _nr.lib().nr_ops_status(index))
