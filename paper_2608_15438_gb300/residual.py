@@ -175,7 +175,7 @@ class ResidualEncoder(torch.nn.Module):
         w = [p.to(_DTYPE) for p in (self.stem[0], self.head[2])]
         blocks = [(p[0], p[1], p[2].to(_DTYPE), p[3], p[4].to(_DTYPE), p[5]) for p in self.blocks]
         out = []
-        for s in range(0, rows.shape[0], batch):
+        for s in range(0, max(rows.shape[0], 1), batch):  # no rows: one empty batch
             r = ops.linear(_rows((rows[s:s + batch].float() * in_scale).to(_DTYPE)), w[0], self.stem[1])
             for g, b, w1, b1, w2, b2 in blocks:
                 r = ops.linear(ops.linear(ops.layer_norm(r, g, b), w1, b1, act=self.act), w2, b2, residual=r)

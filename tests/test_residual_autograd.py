@@ -274,3 +274,11 @@ def test_rows_to_encode_come_in_any_layout():
     model, x = encoder(True), rows(24, 40).T
     assert torch.equal(model(x), model(x.contiguous()))
     assert torch.equal(model.encode(x), model.encode(x.contiguous()))
+
+
+@pytest.mark.parametrize("batch", [1 << 17, 16])
+def test_no_rows_give_no_logits(batch):
+    model = encoder(True)
+    out = model.encode(torch.empty(0, 24), batch=batch)
+    assert out.shape == (0, 6) and out.dtype == torch.float32
+    assert torch.equal(model.encode(rows(40, 24), batch=batch), model.encode(rows(40, 24)))
