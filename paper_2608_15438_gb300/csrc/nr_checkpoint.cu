@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads)
       } else {
         const uint4 h = pack8(p, TypeCode<T>::code);
         const uint32_t w[4] = {h.x, h.y, h.z, h.w};
-        store16x8(y + i * y_ld + j, count, w, prev, next, lanes);
+        store16x8(y + i * y_ld + j, n - j, w, prev, next, lanes);
       }
     }
   }

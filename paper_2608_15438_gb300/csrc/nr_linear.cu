@@ -91,12 +91,12 @@ __device__ __forceinline__ void add_raw(float2 (&v)[4], const uint4 &r, int dtyp
   v[0] = add2(v[0], unpack2(r.x, dtype)), v[1] = add2(v[1], unpack2(r.y, dtype));
   v[2] = add2(v[2], unpack2(r.z, dtype)), v[3] = add2(v[3], unpack2(r.w, dtype));
 }
-// eight 16-bit values of a row, of which `count` are there, the four threads of 32
+// eight 16-bit values of a row that has `left` from p on, the four threads of 32
 // columns together (lanes 4 a .. 4 a + 3 of a warp); vec: at 16-byte addresses
-__device__ __forceinline__ void store_any16(uint16_t *p, int vec, int count, const float2 (&v)[4], int dtype) {
+__device__ __forceinline__ void store_any16(uint16_t *p, int vec, int left, const float2 (&v)[4], int dtype) {
   const int lane = threadIdx.x & 31;
   const uint4 o = pack8(v, dtype);
-  if (vec && count == 8) {
+  if (vec && left >= 8) {
     *reinterpret_cast<uint4 *>(p) = o;
     return;
   }
@@ -104,17 +104,17 @@ __device__ __forceinline__ void store_any16(uint16_t *p, int vec, int count, con
   if (vec) {  // a row's end, which is this lane's alone
 #pragma unroll
     for (int q = 0; q < 7; ++q)
-      if (q < count) p[q] = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
+      if (q < left) p[q] = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
     return;
   }
-  store16x8(p, count, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
+  store16x8(p, left, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
 }
 
 // Finishes s[i, j .. j + 7] (j a multiple of 8; bias: those columns'), row_ok
 // false for rows past the end; called as hold8 is.
 __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, bool row_ok, float2 (&v)[4],
                                         const float2 (&bias)[4]) {
-  const int count = row_ok ? max(0, min(8, (int)E.n - j)) : 0;
+  const int left = row_ok ? (int)E.n - j : 0, count = max(0, min(8, left));
   const uint16_t *pr = static_cast<const uint16_t *>(E.residual) + i * E.residual_ld + j;
   uint32_t res[8];
   if (E.residual) fetch16x8(pr, count, E.residual, E.residual_end, res);
@@ -122,7 +122,7 @@ __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, boo
   for (int q = 0; q < 4; ++q) v[q] = add2(v[q], bias[q]);
   if (E.z) {
     if (E.z_scale) hold8(E, i, j, row_ok, count, v);
-    else store_any16(static_cast<uint16_t *>(E.z) + i * E.z_ld + j, E.z_vec, count, v, E.dtype);
+    else store_any16(static_cast<uint16_t *>(E.z) + i * E.z_ld + j, E.z_vec, left, v, E.dtype);
   }
   if (E.act != NR_ACT_NONE) {
 #pragma unroll
@@ -136,7 +136,7 @@ __device__ __forceinline__ void finish8(const Epilogue &E, int64_t i, int j, boo
     const float o[8] = {v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
     if (count > 0) store8(E.y, i * E.y_ld + j, NR_F32, E.y_vec, count, o);
   } else {
-    store_any16(static_cast<uint16_t *>(E.y) + i * E.y_ld + j, E.y_vec, count, v, E.dtype);
+    store_any16(static_cast<uint16_t *>(E.y) + i * E.y_ld + j, E.y_vec, left, v, E.dtype);
   }
 }
 
@@ -181,7 +181,7 @@ __device__ __forceinline__ void store_block(uint16_t *p, bool there, int lane, c
     if (there) *reinterpret_cast<uint4 *>(p) = o;
   } else {
     const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-    store16x8(p, there ? 8 : 0, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
+    store16x8(p, there ? 32 - 8 * (lane & 3) : 0, w, (lane & 3) > 0, (lane & 3) < 3, 0xfu << (lane & 28));
   }
 }
 

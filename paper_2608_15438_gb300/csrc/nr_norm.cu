@@ -196,7 +196,7 @@ __device__ __forceinline__ void store_row(T *row, int eights, int v, int t, int 
     const uint32_t w[4] = {h.x, h.y, h.z, h.w};
     const int lane = threadIdx.x & 31, at = lane & (kShare - 1);
     const unsigned lanes = kShare == 32 ? 0xffffffffu : ((1u << (kShare & 31)) - 1u) << (lane & ~(kShare - 1));
-    store16x8(row + c, max(0, min(8, n - c)), w, at > 0, at < kShare - 1, lanes);
+    store16x8(row + c, n - c, w, at > 0, at < kShare - 1, lanes);
     return;
   }
   const int st = eights ? 1 : TPR ? TPR : width;

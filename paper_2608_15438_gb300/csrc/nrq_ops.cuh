@@ -153,30 +153,44 @@ __device__ __forceinline__ void settle16x8(const void *p, int count, const void 
   }
   w[0] = o[0], w[1] = o[1], w[2] = o[2], w[3] = o[3];
 }
-// Stores eight 16-bit values from p on, of which `count` are there. The lanes of
-// `lanes` call it together, each eight values after its predecessor's, so that an
-// aligned 16-byte block is a lane's first values after its predecessor's last,
-// and all but the ends are whole blocks. prev, next: the neighbouring lane
-// belongs to the row.
-__device__ __forceinline__ void store16x8(void *p, int count, const uint32_t (&v)[4], bool prev, bool next, unsigned lanes) {
+// What a lane of a row stores of its eight 16-bit values: the aligned 16-byte block
+// of its predecessor's last s values and its own first 8 - s, and its values
+// [from, to) one by one. s: its first value's place in an aligned block; left: the
+// row's values from that one on (past the row's end: 0 or less); prev, next: the
+// neighbouring lane belongs to the row.
+struct Span16x8 {
+  bool block;
+  int from, to;
+};
+__host__ __device__ inline Span16x8 span16x8(int s, int left, bool prev, bool next) {
+  const int count = left < 0 ? 0 : left < 8 ? left : 8, head = 8 - s;
+  Span16x8 w;
+  w.block = (prev || s == 0) && count >= head;
+  w.from = w.block ? head : 0;
+  w.to = s != 0 && next && left - 8 >= head ? head : 8;  // the successor's block holds the lane's last values
+  if (w.to > count) w.to = count;
+  return w;
+}
+// Stores the row's values from p on, at most eight, of which `left` are in the row.
+// The lanes of `lanes` call it together, each eight values after its predecessor's,
+// so that all but the lanes' ends are whole blocks.
+__device__ __forceinline__ void store16x8(void *p, int left, const uint32_t (&v)[4], bool prev, bool next, unsigned lanes) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  const int s = (int)(at & 15) >> 1, head = 8 - s;  // values before the next block
+  const int s = (int)(at & 15) >> 1;
   uint32_t w[8], o[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     w[k] = __shfl_up_sync(lanes, v[k], 1);
     w[k + 4] = v[k];
   }
-  shift_halves(w, head, o);
-  const bool block = (prev || s == 0) && count >= head;
-  if (block) *reinterpret_cast<uint4 *>(at - 2 * (uintptr_t)s) = make_uint4(o[0], o[1], o[2], o[3]);
-  const bool tail = s != 0 && !(next && count - 8 >= head);  // no successor writes this lane's last values
-  if (!block || tail) {
+  shift_halves(w, 8 - s, o);
+  const Span16x8 h = span16x8(s, left, prev, next);
+  if (h.block) *reinterpret_cast<uint4 *>(at - 2 * (uintptr_t)s) = make_uint4(o[0], o[1], o[2], o[3]);
+  if (h.from < h.to) {
     uint16_t *d = static_cast<uint16_t *>(p);
-    const int from = block ? head : 0, to = tail ? 8 : head;
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      if (q >= from && q < to && q < count) d[q] = (uint16_t)(v[q >> 1] >> (16 * (q & 1)));
+      if (q >= h.from && q < h.to) d[q] = (uint16_t)(v[q >> 1] >> (16 * (q & 1)));
   }
 }
 
