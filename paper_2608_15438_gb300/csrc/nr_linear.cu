@@ -449,11 +449,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       };
       multiply(J.p[0], 0, J.items0);
       multiply(J.p[1], J.items0, J.items);
-      // every MMA is complete before tensor memory is freed or the pair ends
       tc::commit<CG>(tc::smem_u32(&B.drain));
-      const uint64_t t0 = tc::now_ns();
-      while (!tc::bar_try(tc::smem_u32(&B.drain), 0) && tc::now_ns() - t0 < (uint64_t)kWaitNs) {
-      }
     }
     __syncwarp();
   } else {
@@ -541,6 +537,13 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   }
   tc::fence_before();
   __syncthreads();
+  if (tid == 0) {
+    // Every MMA is complete before tensor memory is freed; and commits arrive on both
+    // CTAs' barriers, the drain's last, so neither leaves before it has them.
+    const uint64_t t0 = tc::now_ns();
+    while (!tc::bar_try(tc::smem_u32(&B.drain), 0) && tc::now_ns() - t0 < (uint64_t)kWaitNs) {
+    }
+  }
   if (tid == 0 && B.abort) {
     atomicCAS(J.flag, 0, NR_DEV_TIMEOUT);
     // no MMA waits for the copies in flight any more: a millisecond lets them land
