@@ -2,6 +2,8 @@
 // share a power-of-two scale. Bound by memory in both directions: a value's 2 or 4
 // bytes one way and 1 + 1/32 the other. Measured at 262144 x 1536 in bf16: written in
 // 255 us (4.8 TB/s), read in 223 (5.5 TB/s); 65536 x 6144 both in 415 us, 5.9 TB/s.
+// Odd widths shift and share aligned blocks: 200000 x 771 written in 208 us, read in 151
+// (2.3, 3.1 TB/s).
 #include <cuda_runtime.h>
 #include <stdint.h>
 

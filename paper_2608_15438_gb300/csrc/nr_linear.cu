@@ -28,14 +28,19 @@
 // nr_ops_status reports.
 //
 // Measured, bf16: 65536 x 6144 -> 1536 690 to 730 us, 1.7 PFLOP/s (a library's
-// product reaches 1.9); 10000 x 1536 -> 6144 121 us, 155 with GELU and z kept. Bound
-// by shared memory: a stage takes 600 cycles where its MMAs need 512, as copies
-// and operand reads fill its bandwidth.
+// product reaches 1.9); 10000 x 1536 -> 6144 121 us, 154 with GELU and z kept, 173
+// with z in 8 bits, 145 for 136 in the same run with fp32 outputs, whose blocks all
+// take the edges' path. A stage takes 600 cycles where its MMAs need 512, and 512
+// without its copies; but no one rate is filled: of a plain launch's cycles the
+// tensor pipe is active in 72% (64% with GELU and z), shared memory's banks are read
+// in 21% and written in 21%, L2 is busy to 47%.
 //
-// Up to eight rows run on CUDA cores instead (rows_kernel): the weights are
-// read once, which is all the time such a call can take. 1536 -> 6144 takes 6.4
-// us for one row and 15.6 for eight, nine on the tensor cores 13.1; 6144 -> 1536
-// 5.1 and 13.8 against 17.6; 512 -> 512 2.6 and 3.6 against 6.9.
+// Up to eight rows run on CUDA cores instead (rows_kernel), which read the weights
+// once: one to four rows take little more than that, five to eight the code of eight
+// rows. GPU time in us for one, four, five to eight rows, and nine on the tensor
+// cores: 1536 -> 6144 6.0, 8.1, 15.0 and 12.1; 6144 -> 1536 4.8, 8.1, 13.4 and 13.6;
+// 1536 -> 512 2.6, 3.4, 4.6 and 8.3; 512 -> 512 2.3, 2.8, 3.4 and 6.2. So five to
+// eight rows lose to the tensor cores in wide layers and gain in narrow ones.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
@@ -283,8 +288,11 @@ struct Job {
   int64_t wait_ns;
 };
 
-// Items go to the CTAs (pairs) in turns that run forwards and backwards, so that a
-// last, short turn falls to those that had the shorter items.
+// Items go to the CTAs (pairs), the longer first, in turns that run forwards and
+// backwards. A last, short turn falls to those that had the shorter items of the turn
+// before if the number of turns is odd, and to those that had the longer ones if it
+// is even (both products of 4096 rows of 1536 -> 6144: 320 slices on one pair where
+// the mean is 242.5).
 __device__ __forceinline__ int item_at(int turn, int slot, int slots) {
   return turn * slots + ((turn & 1) ? slots - 1 - slot : slot);
 }
@@ -616,7 +624,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 }
 
 // ------------------------------------------------------------ few rows, on CUDA cores
-// Bound by reading the weights: 19 MB of them in 6.4 us at one row, from L2.
+// Bound by reading the weights up to four rows (19 MB of them in 6.0 us at one row, from
+// L2), by conversions and products from five on.
 // A warp holds MR rows against NR columns of C and KS warps share the columns,
 // each a part of t; x's values are converted once for NR weights.
 constexpr int kRowsThreads = 256;
@@ -717,11 +726,17 @@ struct Saved {
 };
 
 // dz = dy act'(z) rounded to T (unless dz is null), and the column sums of the
-// unrounded values over a block's rows -> sums[blockIdx.y] (unless null). Bound
-// by memory: dy and z read, dz written (4096 x 6144 with GELU 24 us, 6.2 TB/s). A block's threads: x over columns, eight
-// each, y over rows; a thread takes four rows at a time (two at other addresses,
-// which take twice the registers), all loads first. VEC: n is a multiple of 8 and dy
-// and z take 16-byte accesses.
+// unrounded values over a block's rows -> sums[blockIdx.y] (unless null). Rounded, as
+// the tensor cores multiply 16-bit operands of one type and dx and dw have w and x of T
+// beside it: dz as a sum of two such terms would double both products. An fp32 dy is
+// rounded there too. In bf16 the rounding takes their error from 0.0017 of the norm,
+// which is their own rounding's, to 0.0023.
+// Bound by memory with z in 16 bits: dy and z read, dz written (4096 x 6144 with GELU 24
+// us, 6.2 TB/s); with z in 8 bits by the arithmetic (16384 x 6144 104 us, 4.9 TB/s, and 95
+// without writing dz, an instruction issued in 69% of cycles). A block's threads: x over columns,
+// eight each, y over rows; a thread takes four rows at a time (two at other addresses,
+// which take twice the registers), all loads first. VEC: n is a multiple of 8 and dy and
+// z take 16-byte accesses.
 constexpr int kDzRows = 4;
 template <bool VEC, typename D, typename T>
 __global__ void __launch_bounds__(256, 3)
@@ -1063,7 +1078,7 @@ struct Scratch {
   }
 };
 
-constexpr int kFewRows = 8;
+constexpr int kFewRows = 8;  // on CUDA cores up to here (figures at the top)
 constexpr int64_t kRowsWarps = 16;  // warps an SM that keep enough of the weights in flight
 
 struct ForwardPlan {

@@ -17,10 +17,14 @@
 // A thread's columns: eight consecutive ones at a time, by 16-byte accesses where
 // every matrix allows them and by shifting pairs of aligned ones where 16-bit rows
 // do not; in fp32 at other addresses single ones a group's width apart, so that a
-// group's accesses stay contiguous. Rows longer than 16384 are read again from memory by a block a row (the long_ kernels).
+// group's accesses stay contiguous. Rows longer than 16384 are read again from memory
+// by a block a row, an element a load (the long_ kernels).
 //
 // Measured (a copy reaches 6.8 TB/s), bf16: forward 262144 x 1536 292 us, 5.5 TB/s;
-// backward 455 us, 5.3 TB/s, with a residual's gradient 592 us, 5.4 TB/s.
+// backward 455 us, 5.3 TB/s, with a residual's gradient 592 us, 5.4 TB/s. From a
+// checkpoint, whose codes become numbers of the type and those fp32, 510 forward and 615
+// backward: x's bytes halve, the time does not. 65536 x 1536 in fp32 159 forward, 207 backward (5.1, 5.8
+// TB/s). 4096 x 20001 in bf16 156 forward, 893 backward (2.1, 0.6 TB/s).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -31,12 +35,13 @@ namespace {
 
 // How the matrices lie. kVec: every eight of a row's columns at a 16-byte address.
 // kPhase: the matrices' rows start at the same distance from 16-byte addresses, as
-// contiguous matrices of any width do. Rows a step (16 bytes' values) apart then start
+// contiguous matrices of one width do, and have at most 4096 columns forward and 8192
+// backward less a step (16 bytes' values). Rows a step apart then start
 // alike, and a block takes only such rows: its threads hold the aligned sixteen bytes
 // of them as in kVec, from `lead` values before a row's first one on, and only a row's
 // ends need care (65536 x 1659 in fp16 against kAny: forward 163 us for 282, backward
 // 201 for 333; 65536 x 3001 in fp32: 337 for 503, 484 for 875).
-// kAny: everything else.
+// kAny: everything else (65536 x 4095 in bf16: forward 509 us).
 enum Lie { kAny, kVec, kPhase };
 template <int A, typename T>
 constexpr int kStepOf = A == kPhase ? 16 / (int)sizeof(T) : 1;
