@@ -86,7 +86,7 @@ def _first(t, name, dtypes):
     if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.is_cuda and t.dim() == 2:
         m, n = t.shape
         ld, inner = t.stride()
-        if 0 < n < 16777216 and (inner == 1 or n == 1):
+        if 0 < n < 16777216 and (inner == 1 or n == 1 or m == 0):
             return m, n, ld, t.get_device()
     _fail(t, name, dtypes, None, None, None)
 
@@ -95,7 +95,7 @@ def _matrix(t, name, dtypes, rows, cols, index):
     """Checks another matrix of the call; its row pitch in elements."""
     if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.get_device() == index and t.shape == (rows, cols):
         ld, inner = t.stride()
-        if inner == 1 or cols == 1:
+        if inner == 1 or cols == 1 or rows == 0:
             return ld
     _fail(t, name, dtypes, rows, cols, index)
 

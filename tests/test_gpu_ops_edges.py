@@ -75,3 +75,19 @@ def test_calls_from_several_threads(ops):
     other.join()
     assert not wrong
     ops.check(0)
+
+
+def test_empty_batches_in_any_layout(ops):
+    """No rows have no strides: slices of a transposed or expanded matrix are taken."""
+    w, b = torch.ones(24, 16, device="cuda", dtype=BF16), torch.ones(24, device="cuda")
+    x, dy = torch.ones(16, 40, device="cuda", dtype=BF16).T[:0], torch.ones(1, 1, device="cuda", dtype=BF16).expand(0, 24)
+    y, z = ops.linear(x, w, b, act="gelu", residual=dy, save="z")
+    assert y.shape == z.shape == (0, 24)
+    dx, dw, db = ops.linear_backward(dy, x, w, z=dy, act="gelu")
+    assert dx.shape == (0, 16) and (dw == 0).all() and (db == 0).all()
+    y, mean, rstd = ops.layer_norm(x, save=True)
+    dx, dw, db = ops.layer_norm_backward(x, x, None, mean, rstd, residual_grad=x)
+    assert y.shape == dx.shape == (0, 16) and (dw == 0).all() and (db == 0).all()
+    assert ops.checkpoint8_read(ops.checkpoint8(x)).shape == (0, 16)
+    with pytest.raises(ValueError, match="stride"):
+        ops.linear(torch.ones(16, 40, device="cuda", dtype=BF16).T, w)
