@@ -558,6 +558,13 @@ def _flat(t, name, dtype, n, index):
     return t
 
 
+def _apart(params):
+    spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size(), i) for i, p in enumerate(params) if p.numel())
+    for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError(f"params[{min(i, j)}] and params[{max(i, j)}] overlap")
+
+
 class AdamWState:
     """What an AdamW step over the tensors `params` keeps (nr_adamw): the averages m
     and v, the step count and, with master, an fp32 master of 16-bit parameters. The
@@ -571,7 +578,7 @@ class AdamWState:
     read back; else they begin with zeros. Every value of the tensors is updated in place."""
 
     __slots__ = ("params", "bits", "master", "m", "v", "step", "at", "size", "_index", "_shapes", "_devices", "_ticket", "_ws_like",
-                 "_table", "_address", "_values", "_types", "_decays")
+                 "_table", "_pointers", "_address", "_values", "_types", "_decays")
 
     def __init__(self, params, bits=32, master=False, m=None, v=None, step=None):
         params = list(params)
@@ -592,10 +599,7 @@ class AdamWState:
             if not p.is_contiguous():
                 raise ValueError(f"{name}: must be contiguous")
             index = p.get_device()
-        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size(), i) for i, p in enumerate(params) if p.numel())
-        for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
-            if begin < end:
-                raise ValueError(f"params[{min(i, j)}] and params[{max(i, j)}] overlap")
+        _apart(params)
         self.params, self.bits, self._index = params, bits, index
         self.at, size = [], 0
         for p in params:
@@ -632,9 +636,10 @@ class AdamWState:
             raise ValueError(f"step: expected a tensor int64 of shape (1,) on cuda:{index}")
         self.step = step
         self._ticket = torch.zeros(1, dtype=torch.int32, device=dev)
-        self._shapes, self._devices = [p.shape for p in params], [index] * len(params)
-        # what a call passes of the tensors (_TENSOR each, then the values' and the gradients' addresses); the first part and
-        # the values' addresses are written anew where they change
+        self._shapes, self._devices = 2 * [p.shape for p in params], 2 * [index] * len(params)  # of the tensors and gradients
+        # what a call passes of them (_TENSOR each, then the values' and the gradients' addresses); the first part is written
+        # anew where it changes
+        self._pointers = struct.Struct(f"{2 * len(params)}q")
         self._table = bytearray((_TENSOR.size + 16) * len(params))
         self._address = ctypes.addressof((ctypes.c_char * len(self._table)).from_buffer(self._table))
         self._values = self._types = self._decays = self._ws_like = None
@@ -645,18 +650,35 @@ class AdamWState:
             out += [t] if self.bits == 32 else t
         return out if self.master is None else [*out, self.master]
 
-    def _look(self):
-        """Parameters that are new, or not where they were at the last step."""
-        for i, p in enumerate(self.params):
-            if p.dtype not in _DT or p.get_device() != self._index or not p.is_contiguous() or p.shape != self._shapes[i]:
-                raise ValueError(f"params[{i}]: changed to a tensor that the state does not fit")
-
-    def _fill(self, types, decays):
-        """Writes the tensors' part of the table, with gradients of `types` (None for none)."""
-        for i, p in enumerate(self.params):
-            _TENSOR.pack_into(self._table, i * _TENSOR.size, p.numel(), self.at[i], _DT[p.dtype],
-                              0 if types[i] is None else _DT[types[i]], decays[i])
-        self._types, self._decays = types, decays
+    def _pass(self, grads, decays):
+        """Checks the tensors and gradients and writes the table; the gradients' types (None for none). A tensor may be
+        another one than at the last step (p.data = ...), at the same address too: all that the kernel goes by is looked at
+        in every call."""
+        count = len(self.params)
+        try:  # all of them at once
+            every = self.params + grads
+            types = [t.dtype for t in every]
+            fit = [t.shape for t in every] == self._shapes and list(map(torch.Tensor.get_device, every)) == self._devices and \
+                all(map(torch.Tensor.is_contiguous, every)) and (types == self._types or _DT.keys() >= set(types))
+        except AttributeError:  # None, or no tensor
+            fit = False
+        if fit:
+            addresses = list(map(torch.Tensor.data_ptr, every))
+        else:
+            for i, p in enumerate(self.params):
+                if p.dtype not in _DT or p.get_device() != self._index or not p.is_contiguous() or p.shape != self._shapes[i]:
+                    raise ValueError(f"params[{i}]: changed to a tensor that the state does not fit")
+            addresses, types = _gradients(grads, self._shapes[:count], self._devices[:count])
+            addresses = [p.data_ptr() for p in self.params] + addresses
+            types = [p.dtype for p in self.params] + types
+        if addresses[:count] != self._values or types != self._types or decays != self._decays:
+            _apart(self.params)
+            for i, p in enumerate(self.params):
+                _TENSOR.pack_into(self._table, i * _TENSOR.size, p.numel(), self.at[i], _DT[types[i]],
+                                  0 if types[count + i] is None else _DT[types[count + i]], decays[i])
+            self._values, self._types, self._decays = addresses[:count], types, decays
+        self._pointers.pack_into(self._table, count * _TENSOR.size, *addresses)
+        return types[count:]
 
 
 def _gradients(grads, shapes, devices):
@@ -729,15 +751,8 @@ def adamw_step(state: AdamWState, grads, lr, betas=(0.9, 0.999), eps=1e-8, weigh
         raise ValueError(f"max_norm: {max_norm}, expected a positive number")
     if not -(1 << 63) <= seed < 1 << 63:
         raise ValueError(f"seed: {seed}, expected a number of 64 bits")
-    values = [p.data_ptr() for p in params]
-    if values != state._values:
-        state._look()
-        state._values, state._types = values, None
-    addresses, types = _gradients(grads, state._shapes, state._devices)
-    if types != state._types or decays != state._decays:
-        state._fill(types, decays)
+    types = state._pass(grads, decays)
     first = count * _TENSOR.size
-    struct.pack_into(f"{2 * count}q", state._table, first, *values, *addresses)
     norm = norm_ptr = ws_ptr = nbytes = 0
     if max_norm is not None:
         norm = torch.empty(1, dtype=torch.float32, device=state.step.device)

@@ -1,0 +1,117 @@
+"""What the AdamW step passes to the library of a state whose parameters have changed, without a GPU: tensors that say
+they are on one, and a stand-in for the library that keeps the table it is given."""
+import ctypes
+import struct
+
+import pytest
+import torch
+
+from paper_2608_15438_gb300 import neuroute as nr
+from paper_2608_15438_gb300 import ops, optim
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+class Library:
+    """Keeps the tensors' rows (n, at, p_dtype, g_dtype, decay, p, g) of the last step."""
+
+    def __init__(self):
+        self.rows, self.calls = None, 0
+
+    def nr_adamw_step(self, packed, index, ws, nbytes, stream):
+        f = ops._ADAMW.unpack(packed)
+        count, tensors, p, g = f[:4]
+        self.rows = [(*ops._TENSOR.unpack(ctypes.string_at(tensors + i * ops._TENSOR.size, ops._TENSOR.size)),
+                      *struct.unpack("q", ctypes.string_at(p + 8 * i, 8)), *struct.unpack("q", ctypes.string_at(g + 8 * i, 8)))
+                     for i in range(count)]
+        self.calls += 1
+        return 0
+
+
+@pytest.fixture
+def library(monkeypatch):
+    fake = Library()
+    monkeypatch.setattr(nr, "lib", lambda: fake)
+    monkeypatch.setattr(ops, "_stream", lambda index: 0)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    return fake
+
+
+def at_the_same_address(p, data):
+    address = p.data_ptr()
+    p.data = data
+    assert p.data_ptr() == address
+
+
+def test_another_layout_at_the_same_address(library):
+    p = torch.nn.Parameter(torch.randn(8, 8))
+    s = ops.AdamWState([p])
+    ops.adamw_step(s, [torch.ones(8, 8)], 1e-3)
+    at_the_same_address(p, p.data.t())
+    for _ in range(2):
+        with pytest.raises(ValueError, match=r"params\[0\]: changed"):
+            ops.adamw_step(s, [torch.ones(8, 8)], 1e-3)
+    assert library.calls == 1
+    at_the_same_address(p, p.data.t())
+    ops.adamw_step(s, [torch.ones(8, 8)], 1e-3)
+    assert library.calls == 2
+    # the optimizer makes its gradients contiguous, whatever the parameters are
+    opt = optim.AdamW([p])
+    p.grad = torch.ones(8, 8)
+    opt.step()
+    at_the_same_address(p, p.data.t())
+    p.grad = torch.ones(8, 8).t()
+    with pytest.raises(ValueError, match="changed"):
+        opt.step()
+
+
+@pytest.mark.parametrize("shape", [(4, 8), (64,), (32,)])
+def test_another_shape_at_the_same_address(library, shape):
+    p = torch.nn.Parameter(torch.randn(64)[:32].view(8, 4))
+    s = ops.AdamWState([p])
+    ops.adamw_step(s, [torch.ones(8, 4)], 1e-3)
+    at_the_same_address(p, torch.as_strided(p.data, shape, torch.empty(shape).stride()))
+    with pytest.raises(ValueError, match="changed"):
+        ops.adamw_step(s, [torch.ones(8, 4)], 1e-3)
+    assert library.calls == 1
+
+
+@pytest.mark.parametrize("old,new", [(F32, BF16), (BF16, F16), (F16, F32)])
+def test_another_type_at_the_same_address(library, old, new):
+    buf = torch.zeros(64)
+    p, q = torch.nn.Parameter(buf.view(old)[:16]), torch.nn.Parameter(torch.zeros(5))
+    s = ops.AdamWState([p, q])
+    grads = [torch.ones(16), torch.ones(5)]
+    for _ in range(2):
+        ops.adamw_step(s, grads, 1e-3)
+        assert [r[2] for r in library.rows] == [ops._DT[old], ops._DT[F32]]
+    at_the_same_address(p, buf.view(new)[:16])
+    for _ in range(2):
+        ops.adamw_step(s, grads, 1e-3)
+        assert [r[:3] for r in library.rows] == [(16, 0, ops._DT[new]), (5, 32, ops._DT[F32])]
+        assert [r[5] for r in library.rows] == [p.data_ptr(), q.data_ptr()]
+
+
+def test_a_device_that_changed(library, monkeypatch):
+    p = torch.nn.Parameter(torch.zeros(8))
+    s = ops.AdamWState([p])
+    ops.adamw_step(s, [torch.ones(8)], 1e-3)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: -1 if t is p else 0)
+    with pytest.raises(ValueError, match="changed"):
+        ops.adamw_step(s, [torch.ones(8)], 1e-3)
+
+
+def test_parameters_that_came_to_overlap(library):
+    buf = torch.zeros(64)
+    p, q = torch.nn.Parameter(buf[:32]), torch.nn.Parameter(buf[32:])
+    s = ops.AdamWState([p, q])
+    grads = [torch.ones(32), torch.ones(32)]
+    ops.adamw_step(s, grads, 1e-3)
+    q.data = buf[16:48]
+    for _ in range(2):
+        with pytest.raises(ValueError, match=r"params\[0\] and params\[1\] overlap"):
+            ops.adamw_step(s, grads, 1e-3)
+    q.data = buf[32:].clone()
+    ops.adamw_step(s, grads, 1e-3)
+    assert library.calls == 2
