@@ -575,7 +575,8 @@ class AdamWState:
 
     params: contiguous CUDA tensors of one device (fp32, fp16 or bf16), none overlapping
     another. m, v, step and a tensor as master are taken as they are, for a state that is
-    read back; else they begin with zeros. Every value of the tensors is updated in place."""
+    read back; else they begin with zeros. Every value of the tensors is updated in place. A parameter may move and
+    change its dtype between steps, but with master not from fp32 to 16 bits: its master is not kept up while it is fp32."""
 
     __slots__ = ("params", "bits", "master", "m", "v", "step", "at", "size", "_index", "_shapes", "_devices", "_ticket", "_ws_like",
                  "_table", "_pointers", "_address", "_values", "_types", "_decays")
@@ -673,6 +674,10 @@ class AdamWState:
             types = [p.dtype for p in self.params] + types
         if addresses[:count] != self._values or types != self._types or decays != self._decays:
             _apart(self.params)
+            if self.master is not None and self._types:  # steps in fp32 have left their master as it was
+                for i in range(count):
+                    if self._types[i] is torch.float32 and types[i] is not torch.float32:
+                        raise ValueError(f"params[{i}]: was fp32 in a step before and has no master of these values")
             for i, p in enumerate(self.params):
                 _TENSOR.pack_into(self._table, i * _TENSOR.size, p.numel(), self.at[i], _DT[types[i]],
                                   0 if types[count + i] is None else _DT[types[count + i]], decays[i])

@@ -115,3 +115,49 @@ def test_parameters_that_came_to_overlap(library):
     q.data = buf[32:].clone()
     ops.adamw_step(s, grads, 1e-3)
     assert library.calls == 2
+
+
+def test_a_master_that_was_not_kept_up(library):
+    """fp32 values have no master of their own to step: one that becomes 16 bits wide later would be stepped from the
+    master of the state's first day."""
+    p, q = torch.nn.Parameter(torch.zeros(8)), torch.nn.Parameter(torch.zeros(8, dtype=BF16))
+    s = ops.AdamWState([p, q], master=True)
+    grads = [torch.ones(8), torch.ones(8)]
+    ops.adamw_step(s, grads, 1e-3)
+    p.data = p.data.bfloat16()
+    for _ in range(2):
+        with pytest.raises(ValueError, match=r"params\[0\]: .* master"):
+            ops.adamw_step(s, grads, 1e-3)
+    p.data = p.data.float()
+    ops.adamw_step(s, grads, 1e-3)
+    # 16 bits of another kind, and fp32 for 16 bits, which takes no master
+    q.data = q.data.half()
+    ops.adamw_step(s, grads, 1e-3)
+    q.data = q.data.float()
+    ops.adamw_step(s, grads, 1e-3)
+    q.data = q.data.half()
+    with pytest.raises(ValueError, match=r"params\[1\]: .* master"):
+        ops.adamw_step(s, grads, 1e-3)
+    assert library.calls == 4
+    # a refused call leaves nothing behind for the next
+    p, q = torch.nn.Parameter(torch.zeros(8, dtype=BF16)), torch.nn.Parameter(torch.zeros(8))
+    s = ops.AdamWState([p, q], master=True)
+    ops.adamw_step(s, grads, 1e-3)
+    want, old = library.rows, (p.data, q.data)
+    p.data, q.data = p.data.view(F16), q.data.half()
+    with pytest.raises(ValueError, match="master"):
+        ops.adamw_step(s, grads, 1e-3)
+    p.data, q.data = old
+    ops.adamw_step(s, grads, 1e-3)
+    assert library.rows == want
+    # before the first step the master has the values that the state was made of
+    p = torch.nn.Parameter(torch.zeros(8))
+    s = ops.AdamWState([p], master=True)
+    p.data = p.data.half()
+    ops.adamw_step(s, [torch.ones(8)], 1e-3)
+    # without masters there is nothing to be out of date
+    p = torch.nn.Parameter(torch.zeros(8))
+    s = ops.AdamWState([p])
+    ops.adamw_step(s, [torch.ones(8)], 1e-3)
+    p.data = p.data.half()
+    ops.adamw_step(s, [torch.ones(8)], 1e-3)
