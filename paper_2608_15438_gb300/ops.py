@@ -729,12 +729,12 @@ def adamw_step(state: AdamWState, grads, lr, betas=(0.9, 0.999), eps=1e-8, weigh
     fp32). seed: of the dither of averages in 8 bits."""
     if not isinstance(state, AdamWState):
         raise TypeError(f"state: expected an AdamWState, got {type(state).__name__}")
+    grads = list(grads)
     if stream is not None:
         return _elsewhere_all(adamw_step, stream, [*state._tensors(), *grads, lr], (state, grads, lr),
                               {"betas": betas, "eps": eps, "weight_decay": weight_decay, "max_norm": max_norm, "seed": seed})
     params, index = state.params, state._index
     count = len(params)
-    grads = list(grads)
     if len(grads) != count:
         raise ValueError(f"grads: {len(grads)}, expected one for each of {count} parameters")
     b1, b2 = betas

@@ -161,3 +161,19 @@ def test_a_master_that_was_not_kept_up(library):
     ops.adamw_step(s, [torch.ones(8)], 1e-3)
     p.data = p.data.half()
     ops.adamw_step(s, [torch.ones(8)], 1e-3)
+
+
+def test_gradients_that_can_be_read_once(library, monkeypatch):
+    """grads and weight_decay as iterators, on the current stream and on another."""
+    import contextlib
+
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    kept = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: kept.append(t.data_ptr()))
+    params, grads = [torch.zeros(8), torch.zeros(5)], [torch.ones(8), torch.ones(5)]
+    s = ops.AdamWState(params)
+    for stream in (None, object()):
+        library.rows = None
+        ops.adamw_step(s, iter(grads), 1e-3, weight_decay=iter([0.1, 0.2]), stream=stream)
+        assert [(r[4], r[6]) for r in library.rows] == [(d, x.data_ptr()) for d, x in zip((0.1, 0.2), grads)]
+    assert {t.data_ptr() for t in params + grads} <= set(kept)
