@@ -558,11 +558,12 @@ def _flat(t, name, dtype, n, index):
     return t
 
 
-def _apart(params):
-    spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size(), i) for i, p in enumerate(params) if p.numel())
+def _apart(named):
+    """Refuses tensors, (name, tensor) each, that share memory."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i) for i, (_, t) in enumerate(named) if t.numel())
     for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
         if begin < end:
-            raise ValueError(f"params[{min(i, j)}] and params[{max(i, j)}] overlap")
+            raise ValueError(f"{named[min(i, j)][0]} and {named[max(i, j)][0]} overlap")
 
 
 class AdamWState:
@@ -574,7 +575,7 @@ class AdamWState:
     parameters' values to begin with. step: int64 [1], the steps taken.
 
     params: contiguous CUDA tensors of one device (fp32, fp16 or bf16), none overlapping
-    another. m, v, step and a tensor as master are taken as they are, for a state that is
+    another or the state's own. m, v, step and a tensor as master are taken as they are, for a state that is
     read back; else they begin with zeros. Every value of the tensors is updated in place. A parameter may move and
     change its dtype between steps, but with master not from fp32 to 16 bits: its master is not kept up while it is fp32."""
 
@@ -600,7 +601,7 @@ class AdamWState:
             if not p.is_contiguous():
                 raise ValueError(f"{name}: must be contiguous")
             index = p.get_device()
-        _apart(params)
+        _apart([(f"params[{i}]", p) for i, p in enumerate(params)])
         self.params, self.bits, self._index = params, bits, index
         self.at, size = [], 0
         for p in params:
@@ -636,6 +637,7 @@ class AdamWState:
         elif not isinstance(step, torch.Tensor) or step.dtype != torch.int64 or step.shape != (1,) or step.get_device() != index:
             raise ValueError(f"step: expected a tensor int64 of shape (1,) on cuda:{index}")
         self.step = step
+        _apart(self._named())
         self._ticket = torch.zeros(1, dtype=torch.int32, device=dev)
         self._shapes, self._devices = 2 * [p.shape for p in params], 2 * [index] * len(params)  # of the tensors and gradients
         # what a call passes of them (_TENSOR each, then the values' and the gradients' addresses); the first part is written
@@ -644,6 +646,13 @@ class AdamWState:
         self._table = bytearray((_TENSOR.size + 16) * len(params))
         self._address = ctypes.addressof((ctypes.c_char * len(self._table)).from_buffer(self._table))
         self._values = self._types = self._decays = self._ws_like = None
+
+    def _named(self):
+        """All tensors that a step writes, with their names."""
+        out = [(f"params[{i}]", p) for i, p in enumerate(self.params)]
+        for name, t in (("m", self.m), ("v", self.v)):
+            out += [(name, t)] if self.bits == 32 else [(name, t[0]), (name + "'s scales", t[1])]
+        return out + [("step", self.step)] + ([] if self.master is None else [("master", self.master)])
 
     def _tensors(self):
         out = [*self.params, self.step, self._ticket]
@@ -673,7 +682,8 @@ class AdamWState:
             addresses = [p.data_ptr() for p in self.params] + addresses
             types = [p.dtype for p in self.params] + types
         if addresses[:count] != self._values or types != self._types or decays != self._decays:
-            _apart(self.params)
+            if addresses[:count] != self._values or types != self._types:
+                _apart(self._named())
             if self.master is not None and self._types:  # steps in fp32 have left their master as it was
                 for i in range(count):
                     if self._types[i] is torch.float32 and types[i] is not torch.float32:

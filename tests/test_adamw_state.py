@@ -177,3 +177,24 @@ def test_gradients_that_can_be_read_once(library, monkeypatch):
         ops.adamw_step(s, iter(grads), 1e-3, weight_decay=iter([0.1, 0.2]), stream=stream)
         assert [(r[4], r[6]) for r in library.rows] == [(d, x.data_ptr()) for d, x in zip((0.1, 0.2), grads)]
     assert {t.data_ptr() for t in params + grads} <= set(kept)
+
+
+def test_arrays_of_a_state_that_overlap(library):
+    p = torch.zeros(64)
+    flat, step = torch.zeros(128), torch.zeros(1, dtype=torch.int64)
+    u8 = torch.zeros(256, dtype=torch.uint8)
+    for kw, match in [(dict(m=flat[:64], v=flat[:64]), "m and v"), (dict(m=flat[:64], v=flat[32:96]), "m and v"),
+                      (dict(v=p), r"params\[0\] and v"), (dict(master=flat[:64], m=flat[60:124]), "m and master"),
+                      (dict(m=flat[:64], step=flat[62:64].view(torch.int64)), "m and step"),
+                      (dict(bits=8, m=(u8[:64], u8[64:66]), v=(u8[64:128], u8[200:202])), "m's scales and v"),
+                      (dict(bits=8, m=(u8[:64], u8[64:66]), v=(u8[80:144], u8[65:67])), "m's scales and v's scales")]:
+        with pytest.raises(ValueError, match=f"{match} overlap"):
+            ops.AdamWState([p], **kw)
+    s = ops.AdamWState([p], m=flat[:64], v=flat[64:], step=step)
+    ops.adamw_step(s, [torch.ones(64)], 1e-3)
+    q = torch.nn.Parameter(torch.zeros(64))
+    s = ops.AdamWState([q], m=flat[:64], v=flat[64:])
+    q.data = flat[:64]
+    with pytest.raises(ValueError, match=r"params\[0\] and m overlap"):
+        ops.adamw_step(s, [torch.ones(64)], 1e-3)
+    ops.AdamWState([torch.zeros(0)], bits=8, m=(u8[:0], u8[:0]), v=(u8[:0], u8[:0]))
