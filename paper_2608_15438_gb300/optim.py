@@ -44,15 +44,19 @@ class AdamW:
         for p in self.params:
             p.grad = None
 
+    def _shapes(self):
+        return [tuple(p.shape) for p in self.params]
+
     def state_dict(self):
-        """The averages, masters, step count and settings; the tensors are the optimizer's own."""
+        """The averages, masters, step count, settings and the parameters' shapes and dtypes; the tensors are the
+        optimizer's own."""
         s = self.state
-        return {"bits": s.bits, "m": s.m, "v": s.v, "master": s.master, "step": s.step, "lr": self.lr, "betas": self.betas,
-                "eps": self.eps, "weight_decay": self.weight_decay, "max_norm": self.max_norm, "seed": self.seed}
+        return {"bits": s.bits, "shapes": self._shapes(), "dtypes": [p.dtype for p in self.params], "m": s.m, "v": s.v,
+                "master": s.master, "step": s.step, "lr": self.lr, "betas": self.betas, "eps": self.eps, "weight_decay": self.weight_decay, "max_norm": self.max_norm, "seed": self.seed}
 
     @torch.no_grad()
     def load_state_dict(self, d):
-        """Takes over what state_dict gave, of an optimizer over tensors of the same sizes; copies."""
+        """Takes over what state_dict gave, of an optimizer over tensors of the same shapes in the same order; copies."""
         s = self.state
         if d["bits"] != s.bits or (d["master"] is None) != (s.master is None):
             raise ValueError(f"state: averages in {d['bits']} bits {'without' if d['master'] is None else 'with'} masters, "
@@ -60,8 +64,12 @@ class AdamW:
         pairs = [(s.step, d["step"])] + ([] if s.master is None else [(s.master, d["master"])])
         for mine, theirs in ((s.m, d["m"]), (s.v, d["v"])):
             pairs += [(mine, theirs)] if s.bits == 32 else list(zip(mine, theirs))
-        if len(d["weight_decay"]) != len(self.params) or any(a.shape != b.shape for a, b in pairs):
+        # without shapes, as before they were saved: by the number of tensors and the sum of their sizes
+        if [tuple(x) for x in d.get("shapes", self._shapes())] != self._shapes() or len(d["weight_decay"]) != len(self.params) or \
+                any(a.shape != b.shape for a, b in pairs):
             raise ValueError("state: made for tensors of other sizes")
+        if s.master is not None and any(a is torch.float32 and p.dtype is not a for a, p in zip(d.get("dtypes", []), self.params)):
+            raise ValueError("state: made for fp32 tensors, which keep no masters, where these have 16 bits")
         for a, b in pairs:
             a.copy_(b)
         for k in ("lr", "betas", "eps", "weight_decay", "max_norm", "seed"):
