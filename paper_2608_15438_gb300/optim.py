@@ -52,7 +52,8 @@ class AdamW:
         optimizer's own."""
         s = self.state
         return {"bits": s.bits, "shapes": self._shapes(), "dtypes": [p.dtype for p in self.params], "m": s.m, "v": s.v,
-                "master": s.master, "step": s.step, "lr": self.lr, "betas": self.betas, "eps": self.eps, "weight_decay": self.weight_decay, "max_norm": self.max_norm, "seed": self.seed}
+                "master": s.master, "step": s.step, "lr": self.lr, "betas": self.betas, "eps": self.eps,
+                "weight_decay": list(self.weight_decay), "max_norm": self.max_norm, "seed": self.seed}
 
     @torch.no_grad()
     def load_state_dict(self, d):
@@ -72,8 +73,13 @@ class AdamW:
             raise ValueError("state: made for fp32 tensors, which keep no masters, where these have 16 bits")
         for a, b in pairs:
             a.copy_(b)
-        for k in ("lr", "betas", "eps", "weight_decay", "max_norm", "seed"):
+        for k in ("betas", "eps", "max_norm", "seed"):
             setattr(self, k, d[k])
+        self.weight_decay = list(d["weight_decay"])
+        if isinstance(d["lr"], torch.Tensor) and isinstance(self.lr, torch.Tensor):
+            self.lr.copy_(d["lr"])  # where a captured step reads it
+        else:
+            self.lr = d["lr"].to(s.step.device, copy=True) if isinstance(d["lr"], torch.Tensor) else d["lr"]
 
 
 def of(name, params, lr, weight_decay=0.0, max_norm=None):

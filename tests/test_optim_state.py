@@ -59,3 +59,21 @@ def test_masters_of_fp32_tensors_are_refused():
     with pytest.raises(ValueError, match="masters"):
         of(BF16, BF16).load_state_dict(of(BF16, F32).state_dict())
     of(F32, F32).load_state_dict(of(F32, F32).state_dict())
+
+
+def test_settings_are_copies():
+    """Neither optimizer sees what is set on the other afterwards; a rate in a tensor, which a captured step reads, stays
+    where it is."""
+    a, b = over((8, 4), 5, weight_decay=0.1, lr=torch.tensor([1e-3])), over((8, 4), 5, lr=5.0)
+    saved = a.state_dict()
+    b.load_state_dict(saved)
+    assert b.weight_decay == [0.1, 0.0] and float(b.lr) == float(torch.tensor(1e-3))
+    a.weight_decay[0], b.weight_decay[1] = 0.7, 0.3
+    a.lr.fill_(9.0)
+    assert saved["weight_decay"] == [0.1, 0.0]
+    assert (a.weight_decay, b.weight_decay) == ([0.7, 0.0], [0.1, 0.3]) and float(b.lr) < 1.0
+    at = b.lr
+    b.load_state_dict(a.state_dict())
+    assert b.lr is at and float(at) == 9.0
+    b.load_state_dict(over((8, 4), 5, lr=2.0).state_dict())
+    assert b.lr == 2.0
