@@ -53,6 +53,7 @@ struct Step {
   const double *parts;  // sums of squares
   int part_count;
   int counts;  // the launch that ends the step
+  int tiny;
   uint32_t key0, key1;
 };
 
@@ -335,8 +336,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double *parts, int
 }
 
 // ------------------------------------------------------------ the step
-// rate m / (v^1/2 root + eps) by the hardware's approximations, 2^-22 of it. TINY: for an eps that a root of a v
-// below fp32's normal numbers (2^-63) could matter beside; those that flush them cost eight instructions less.
+// rate m / (v^1/2 root + eps) by the hardware's approximations, 2^-22 of it. TINY (tiny_matters): for an eps that a
+// root of a v below fp32's normal numbers could matter beside; those that flush them cost eight instructions less.
 template <bool TINY>
 __device__ __forceinline__ float2 quotient(float2 m, float2 v, float rate, float root, float eps) {
   float2 r;
@@ -347,7 +348,6 @@ __device__ __forceinline__ float2 quotient(float2 m, float2 v, float rate, float
   else asm("rcp.approx.ftz.f32 %0, %2;\n rcp.approx.ftz.f32 %1, %3;\n" : "=f"(r.x), "=f"(r.y) : "f"(d.x), "f"(d.y));
   return mul2(mul2(m, both(rate)), r);
 }
-constexpr float kTinyEps = 1e-12f;  // 2^-63 root is below 2^-24 of it for beta2 up to 1 - 1e-9
 
 // A thread takes eight consecutive values at a time; four lanes share a group of the 8-bit form. Blocks an SM by the
 // registers: 64 a thread and four in fp32; 8 bits want 80 (four blocks spill: 735 us for 655; two with the next
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED && BITS == 32 ? 4 : 3)
       }
     }
     const float keep = S.lr_at ? 1.0f - lr * e.decay : e.decay;
-    if (S.eps < kTinyEps) {
+    if (S.tiny) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) p[q] = fma2(p[q], both(keep), quotient<true>(m[q], v[q], -rate, root, S.eps));
     } else {
@@ -592,6 +592,10 @@ int grid_of(uint32_t chunks, int sms, int per_sm) {
   return (int)(chunks < most ? chunks : most);
 }
 
+// Whether v below 2^-126, whose root is below 2^-63, can move a denominator by 2^-24 of it: root is (1 - beta2^t)^-1/2,
+// largest at the first step.
+bool tiny_matters(const nr_adamw *a) { return a->eps < ldexp(1.0, -39) / sqrt(1.0 - a->beta2); }
+
 // blocks' sums of squares -> parts; how many
 template <int CAP>
 cudaError_t squares(const nr_adamw *a, int sms, double *parts, int &count, cudaStream_t s) {
@@ -671,6 +675,7 @@ extern "C" nr_status nr_adamw_step(const nr_adamw *a, int device, void *ws, int6
   S.c2 = (float)(1.0 - a->beta2);
   S.eps = fmaxf((float)a->eps, 1.17549435e-38f);  // its reciprocal is in fp32's range
   S.one = 1.0f;
+  S.tiny = tiny_matters(a);
   S.key0 = (uint32_t)a->seed;
   S.key1 = (uint32_t)((uint64_t)a->seed >> 32);
   cudaError_t e = cudaSuccess;

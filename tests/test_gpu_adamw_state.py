@@ -1,4 +1,4 @@
-"""AdamW states whose parameters become other tensors between steps."""
+"""AdamW states whose parameters become other tensors between steps, and averages and norms at the ends of fp32's range."""
 import pytest
 
 from gpu_util import need_cuda
@@ -53,3 +53,33 @@ def test_a_transposed_parameter_is_refused(ops):
     with pytest.raises(ValueError, match="does not fit"):
         opt.step()
     assert torch.equal(p.detach(), before.t()) and int(opt.state.step) == 1
+
+
+@pytest.mark.parametrize("bits,offset", [(32, 0), (32, 1), (8, 0), (8, 1)])
+@pytest.mark.parametrize("eps", [1e-20, 1e-12, 2e-11, 5.7e-11, 5.8e-11, 1e-8])
+@pytest.mark.parametrize("b2", [0.0, 0.95, 0.999, 1 - 1e-6])
+@pytest.mark.parametrize("t", [1, 5])
+def test_averages_below_the_normal_numbers(ops, bits, offset, eps, b2, t):
+    """Squares of gradients down to nothing: their root counts beside eps however small it is. m' and v' are those that
+    the step holds to (three roundings, from zeros one and two); the update from them is allowed 2^-20 of itself, as
+    elsewhere: 1 - beta^t good to 2^-22, root and reciprocal, four roundings."""
+    import math
+
+    import numpy as np
+
+    f, n, b1, lr = np.float32, 4096, 0.9, 1e-2
+    rng = np.random.default_rng(int(1e3 * b2) + t)
+    x = (10.0 ** rng.uniform(-23.0, -15.0, n) * rng.choice([-1.0, 1.0], n)).astype(f)
+    grads, params = torch.zeros(n + offset, device="cuda")[offset:], torch.zeros(n + offset, device="cuda")[offset:]
+    grads.copy_(torch.from_numpy(x))
+    s = ops.AdamWState([params], bits=bits)
+    s.step.fill_(t - 1)
+    ops.adamw_step(s, [grads], lr, betas=(b1, b2), eps=eps, weight_decay=0.0)
+    m, v = f(1 - b1) * x, (f(1 - b2) * x) * x
+    assert (v < 2.0 ** -126).any() and (v > 2.0 ** -126).any()
+    if bits == 32:
+        assert np.array_equal(s.m.cpu().numpy(), m) and np.array_equal(s.v.cpu().numpy(), v)
+    root = 1.0 if b2 == 0.0 else math.sqrt(-1.0 / math.expm1(t * math.log(b2)))
+    want = -lr / -math.expm1(t * math.log(b1)) * m.astype(np.float64) / (np.sqrt(v.astype(np.float64)) * root + eps)
+    got = params.cpu().numpy().astype(np.float64)
+    assert (np.abs(got - want) <= 2.0 ** -20 * np.abs(want)).all()
