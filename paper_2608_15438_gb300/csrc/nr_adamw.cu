@@ -260,18 +260,26 @@ __device__ __forceinline__ double block_sum(double v, double *shared) {
 
 // Loads of kAtOnce chunks are under way together (one at a time: 2.2 TB/s). Sixteen squares a thread are
 // added in fp32, their sums in two fp32 numbers, the second what the first's roundings lose (Knuth's exact sum of
-// two): the few fp64 units would bind.
+// two): the few fp64 units would bind. Sums that near fp32's end go on in fp64, so that however many gradients
+// below 2^60 there are, whose sixteen squares are below 2^124, none is infinite.
 template <int CAP, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) square_kernel(const __grid_constant__ Table<CAP> T, double *parts) {
   constexpr int kAtOnce = 4;
-  __shared__ double shared[kThreads / 32];
+  __shared__ double shared[kThreads / 32], past[kThreads];  // a thread's own
   float high = 0.0f, low = 0.0f;
+  past[threadIdx.x] = 0.0;
+  // an infinity stays one (its second number is NaN)
+  const auto sum = [&] { return past[threadIdx.x] + (high < INFINITY ? (double)high + (double)low : (double)high); };
   const auto add = [&](float2 s) {
     const float v = s.x + s.y, next = high + v, of = next - high;
     low += (high - (next - of)) + (v - of);
     high = next;
   };
   for (uint32_t c0 = blockIdx.x * kAtOnce; c0 < T.chunks; c0 += gridDim.x * kAtOnce) {
+    if (__builtin_expect(high >= 0x1p126f, 0)) {
+      past[threadIdx.x] = sum();
+      high = low = 0.0f;
+    }
     int k = find(T, c0, T.count - 1);
     const Entry &e = T.e[k];
     const int64_t j = (int64_t)(c0 - e.first) * kChunk;
@@ -321,9 +329,8 @@ __global__ void __launch_bounds__(kThreads) square_kernel(const __grid_constant_
       add(s);
     }
   }
-  // an infinity stays one (its second number is NaN)
-  const double sum = block_sum(high < INFINITY ? (double)high + (double)low : (double)high, shared);
-  if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+  const double all = block_sum(sum(), shared);
+  if (threadIdx.x == 0) parts[blockIdx.x] = all;
 }
 
 __global__ void __launch_bounds__(kThreads) norm_kernel(const double *parts, int count, float *norm) {

@@ -83,3 +83,25 @@ def test_averages_below_the_normal_numbers(ops, bits, offset, eps, b2, t):
     want = -lr / -math.expm1(t * math.log(b1)) * m.astype(np.float64) / (np.sqrt(v.astype(np.float64)) * root + eps)
     got = params.cpu().numpy().astype(np.float64)
     assert (np.abs(got - want) <= 2.0 ** -20 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype,offset", [(F32, 0), (BF16, 0), (F32, 1), (BF16, 1)])
+@pytest.mark.parametrize("n", [1000, 1 << 20, (1 << 27) + 77])
+def test_norms_of_gradients_near_two_to_the_60(ops, n, dtype, offset):
+    """Gradients below 2^60, many of them: their squares' sum is past fp32's range, the norm is not."""
+    top = 2.0 ** 60 * (1 - 2.0 ** -8)
+    x = torch.full((n + offset,), top, device="cuda", dtype=dtype)[offset:]
+    x[::2].neg_()
+    x[:7] = 1.0
+    want = top * (n - 7) ** 0.5
+    assert abs(float(ops.grad_norm([x])) - want) <= 2.0 ** -20 * want
+    p = torch.zeros(n + offset, device="cuda", dtype=BF16)[offset:]
+    s = ops.AdamWState([p])
+    norm = ops.adamw_step(s, [x], 1e-3, max_norm=1.0, weight_decay=0.0)
+    assert abs(float(norm) - want) <= 2.0 ** -20 * want and int(s.step) == 1
+    m = 0.1 * top / want
+    assert abs(float(s.m[8]) + m) <= 2.0 ** -18 * m and abs(float(s.m[9]) - m) <= 2.0 ** -18 * m
+    x[n // 2] = float("inf")
+    assert not float(ops.grad_norm([x])) < float("inf")
+    x[n // 2] = float("nan")
+    assert not float(ops.grad_norm([x])) < float("inf")
