@@ -105,3 +105,37 @@ def test_norms_of_gradients_near_two_to_the_60(ops, n, dtype, offset):
     assert not float(ops.grad_norm([x])) < float("inf")
     x[n // 2] = float("nan")
     assert not float(ops.grad_norm([x])) < float("inf")
+
+
+def test_steps_from_several_threads(ops):
+    """Each on a state and a stream of its own."""
+    import threading
+
+    def states(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        params = [torch.randn(k, generator=g, device="cuda") for k in (70000 + seed, 33)]
+        grads = [torch.randn(p.shape, generator=g, device="cuda") for p in params]
+        return ops.AdamWState(params, bits=8 if seed % 2 else 32), grads
+
+    def steps(seed, state, grads):
+        for _ in range(40):
+            ops.adamw_step(state, grads, 1e-3, max_norm=0.1 * (seed + 1), seed=seed)
+
+    want = [states(i) for i in range(4)]
+    for i, w in enumerate(want):
+        steps(i, *w)
+    got = [states(i) for i in range(4)]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            steps(i, *got[i])
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for (a, _), (b, _) in zip(got, want):
+        assert int(a.step) == 40 and all(torch.equal(x, y) for x, y in zip(a._tensors(), b._tensors()))
