@@ -439,7 +439,8 @@ def block_norm(r, u=None, gate=None, gate_act="sigmoid", scale=None, alpha=1.0, 
     post and pre: "none", "rms" or "layer"; without pre h is None. u [m x n] and gate [m x n] or [m x 1] (its
     argument) in fp32, fp16 or bf16; r [m x n] in that dtype or fp32. The vectors [n] in u's dtype or fp32, all the
     same; each may be None. Without u, y is r itself and h, in out_dtype (r's by default), pre(r) weight +
-    bias. save: (y, h, stats), stats what block_norm_backward takes (None where there is no norm)."""
+    bias. save: (y, h, stats), stats what block_norm_backward takes (None where there is no norm). Backward has a 16-bit
+    y only as rounded; streams whose mean is large beside their deviation are for fp32."""
     if stream is not None:
         return _elsewhere(block_norm, stream, (r, u),
                           {"gate": gate, "gate_act": gate_act, "scale": scale, "alpha": alpha, "post": post,

@@ -256,7 +256,7 @@ class GatedEncoder(torch.nn.Module):
         E(x) = W_h h_n + b_h.
     norm and post: "rms" or "layer" (post also "none"), with weights, layer norms with biases too. gate: "none",
     "row" (q one number a row) or "full". scale: a vector that begins with this value, or None. stream32 keeps r
-    in fp32."""
+    in fp32, for streams that move away from zero: gradients are made from r as stored."""
 
     def __init__(self, D: int, width: int, blocks: int, b: int, expand: int = 4, act: str = "gelu", norm: str = "rms",
                  post: str = "rms", gate: str = "full", scale=None, stream32: bool = False, hold8: bool = True,
