@@ -71,6 +71,7 @@ class Checkpoint8:
 _HALF = (torch.float16, torch.bfloat16)
 _FLOATS = tuple(_DT)
 _stream = torch._C._cuda_getCurrentRawStream  # the current stream of a device index, as an integer
+_address, _contiguous = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
 
 
 def _fail(t, name, dtypes, rows, cols, index):
@@ -580,8 +581,8 @@ class AdamWState:
     read back; else they begin with zeros. Every value of the tensors is updated in place. A parameter may move and
     change its dtype between steps, but with master not from fp32 to 16 bits: its master is not kept up while it is fp32."""
 
-    __slots__ = ("params", "bits", "master", "m", "v", "step", "at", "size", "_index", "_shapes", "_devices", "_ticket", "_ws_like",
-                 "_table", "_pointers", "_address", "_values", "_types", "_decays")
+    __slots__ = ("params", "bits", "master", "m", "v", "step", "at", "size", "_index", "_shapes", "_device", "_ticket", "_one",
+                 "_ws_like", "_table", "_pointers", "_address", "_values", "_types", "_decays")
 
     def __init__(self, params, bits=32, master=False, m=None, v=None, step=None):
         params = list(params)
@@ -639,8 +640,8 @@ class AdamWState:
             raise ValueError(f"step: expected a tensor int64 of shape (1,) on cuda:{index}")
         self.step = step
         _apart(self._named())
-        self._ticket = torch.zeros(1, dtype=torch.int32, device=dev)
-        self._shapes, self._devices = 2 * [p.shape for p in params], 2 * [index] * len(params)  # of the tensors and gradients
+        self._ticket, self._one = torch.zeros(1, dtype=torch.int32, device=dev), torch.empty(1, device=dev)
+        self._shapes, self._device = 2 * [p.shape for p in params], {index}  # of the tensors and gradients
         # what a call passes of them (_TENSOR each, then the values' and the gradients' addresses); the first part is written
         # anew where it changes
         self._pointers = struct.Struct(f"{2 * len(params)}q")
@@ -662,28 +663,31 @@ class AdamWState:
         return out if self.master is None else [*out, self.master]
 
     def _pass(self, grads, decays):
-        """Checks the tensors and gradients and writes the table; the gradients' types (None for none). A tensor may be
+        """Checks the tensors and gradients and writes the table; returns the tensors that have a gradient. A tensor may be
         another one than at the last step (p.data = ...), at the same address too: all that the kernel goes by is looked at
         in every call."""
         count = len(self.params)
         try:  # all of them at once
             every = self.params + grads
             types = [t.dtype for t in every]
-            fit = [t.shape for t in every] == self._shapes and list(map(torch.Tensor.get_device, every)) == self._devices and \
-                all(map(torch.Tensor.is_contiguous, every)) and (types == self._types or _DT.keys() >= set(types))
-        except AttributeError:  # None, or no tensor
+            same = types == self._types
+            fit = [t.shape for t in every] == self._shapes and set(map(torch.Tensor.get_device, every)) == self._device and \
+                all(map(_contiguous, every)) and (same or _DT.keys() >= set(types))
+        except (AttributeError, TypeError):  # None, or no tensor
             fit = False
         if fit:
-            addresses = list(map(torch.Tensor.data_ptr, every))
+            addresses = list(map(_address, every))
+            values = addresses[:count]
         else:
             for i, p in enumerate(self.params):
                 if p.dtype not in _DT or p.get_device() != self._index or not p.is_contiguous() or p.shape != self._shapes[i]:
                     raise ValueError(f"params[{i}]: changed to a tensor that the state does not fit")
-            addresses, types = _gradients(grads, self._shapes[:count], self._devices[:count])
-            addresses = [p.data_ptr() for p in self.params] + addresses
-            types = [p.dtype for p in self.params] + types
-        if addresses[:count] != self._values or types != self._types or decays != self._decays:
-            if addresses[:count] != self._values or types != self._types:
+            addresses, types = _gradients(grads, self._shapes[:count], [self._index] * count)
+            values = [p.data_ptr() for p in self.params]
+            addresses, types = values + addresses, [p.dtype for p in self.params] + types
+            same = types == self._types
+        if not same or values != self._values or decays is not self._decays:
+            if not same or values != self._values:
                 _apart(self._named())
             if self.master is not None and self._types:  # steps in fp32 have left their master as it was
                 for i in range(count):
@@ -692,9 +696,9 @@ class AdamWState:
             for i, p in enumerate(self.params):
                 _TENSOR.pack_into(self._table, i * _TENSOR.size, p.numel(), self.at[i], _DT[types[i]],
                                   0 if types[count + i] is None else _DT[types[count + i]], decays[i])
-            self._values, self._types, self._decays = addresses[:count], types, decays
+            self._values, self._types, self._decays = values, types, decays
         self._pointers.pack_into(self._table, count * _TENSOR.size, *addresses)
-        return types[count:]
+        return self.params if fit else [p for p, g in zip(self.params, grads) if g is not None]
 
 
 def _gradients(grads, shapes, devices):
@@ -754,10 +758,12 @@ def adamw_step(state: AdamWState, grads, lr, betas=(0.9, 0.999), eps=1e-8, weigh
     if not eps > 0.0:
         raise ValueError(f"eps: {eps}, expected a positive number")
     decays = [weight_decay] * count if isinstance(weight_decay, (int, float)) else list(weight_decay)
-    if decays != state._decays and (len(decays) != count or not all(0.0 <= d <= _MOST for d in decays)):
+    if decays == state._decays:
+        decays = state._decays
+    elif len(decays) != count or not all(0.0 <= d <= _MOST for d in decays):
         raise ValueError("weight_decay: expected a number that is not negative, or one for each parameter")
     lr_at = 0
-    if isinstance(lr, torch.Tensor):
+    if type(lr) is not float and isinstance(lr, torch.Tensor):
         if lr.dtype != torch.float32 or lr.numel() != 1 or lr.get_device() != index:
             raise ValueError(f"lr: expected a number or one fp32 value on cuda:{index}")
         lr_at, lr = lr.data_ptr(), 0.0
@@ -767,11 +773,11 @@ def adamw_step(state: AdamWState, grads, lr, betas=(0.9, 0.999), eps=1e-8, weigh
         raise ValueError(f"max_norm: {max_norm}, expected a positive number")
     if not -(1 << 63) <= seed < 1 << 63:
         raise ValueError(f"seed: {seed}, expected a number of 64 bits")
-    types = state._pass(grads, decays)
+    moved = state._pass(grads, decays)
     first = count * _TENSOR.size
     norm = norm_ptr = ws_ptr = nbytes = 0
     if max_norm is not None:
-        norm = torch.empty(1, dtype=torch.float32, device=state.step.device)
+        norm = torch.empty_like(state._one)  # made the shorter way
         norm_ptr = norm.data_ptr()
     at = state._address
     if state.bits == 32:
@@ -785,12 +791,12 @@ def adamw_step(state: AdamWState, grads, lr, betas=(0.9, 0.999), eps=1e-8, weigh
     if norm_ptr:
         if state._ws_like is None:
             state._ws_like, _ = _scratch("nr_adamw_step", lib.nr_adamw_workspace(packed, index), state.step.device)
-        ws = torch.empty_like(state._ws_like)  # a call's own, as its stream may be; made the shorter way
+        ws = torch.empty_like(state._ws_like)  # a call's own, as its stream may be
         ws_ptr, nbytes = ws.data_ptr(), ws.numel()
     st = lib.nr_adamw_step(packed, index, ws_ptr, nbytes, _stream(index))
     if st:
         raise _nr.NRError("nr_adamw_step", st)
-    torch.autograd.graph.increment_version(params if None not in types else [p for p, t in zip(params, types) if t is not None])
+    torch.autograd.graph.increment_version(moved)
     return norm if norm_ptr else None
 
 

@@ -198,3 +198,15 @@ def test_arrays_of_a_state_that_overlap(library):
     with pytest.raises(ValueError, match=r"params\[0\] and m overlap"):
         ops.adamw_step(s, [torch.ones(64)], 1e-3)
     ops.AdamWState([torch.zeros(0)], bits=8, m=(u8[:0], u8[:0]), v=(u8[:0], u8[:0]))
+
+
+def test_gradients_that_are_no_tensors(library):
+    import numpy as np
+
+    s = ops.AdamWState([torch.zeros(8), torch.zeros(5)])
+    for bad in (np.ones(5, np.float32), [1.0] * 5, 1.0):
+        with pytest.raises(TypeError, match=r"grads\[1\]: expected a torch.Tensor"):
+            ops.adamw_step(s, [torch.ones(8), bad], 1e-3)
+    assert library.calls == 0
+    ops.adamw_step(s, [None, torch.ones(5)], 1e-3)
+    assert [r[6] != 0 for r in library.rows] == [False, True]
