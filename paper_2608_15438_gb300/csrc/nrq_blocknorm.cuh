@@ -1,7 +1,8 @@
 // The norms around a block of a residual encoder (nr_block_norm): rows of up to 8192
 // columns, worked on in shared memory. Bound by memory: forward reads r, u and the gate and writes y and h,
 // backward reads dh, dy, y, u and the gate and writes dr, du and dgate, each once. Of 6.8 TB/s measured:
-//   forward   262144 x 1536 bf16 around an fp32 stream 733 us, 6.6 TB/s; 10000 x 1536 bf16 30 us, 5.1 (two waves of rows)
+//   forward   262144 x 1536 bf16 around an fp32 stream 733 us, 6.6 TB/s; 10000 x 1536 bf16 30 us, 5.1 (eleven
+//             warps an SM, six rows each: beginning and end)
 //   backward  65536 x 1536 bf16 286 us, 5.6 TB/s (an instruction issued in 47% of cycles, twelve warps an SM: their
 //             160 registers hold the columns' sums); 30011 x 387 fp32 71 us, 3.9, and 81 written at another pitch: 168
 //             registers leave eleven warps, and what a row costs is shared by 387 columns (two warps a row, eight
@@ -63,7 +64,8 @@ __device__ __forceinline__ float vec(const void *p, int64_t j, int dtype, float 
 // ------------------------------------------------------------ rows in shared memory
 // A row is taken by TPR lanes of a warp, or by several warps (TPR 0), 8 V columns a
 // thread: V eights where all matrices have 16 bits, else 2 V pieces of four, neighbouring threads' pieces side by
-// side. Copies of the rows to come are under way (cp.async) while one is worked on. What a row costs whatever
+// side. Copies of the rows to come are under way (cp.async) while one is worked on: long rows have one stage a
+// group, whose next copy starts when the present row is in registers, short and few ones up to four. What a row costs whatever
 // its length (addresses, exchanges, statistics: some 200 instructions a warp) is shared by a thread's columns: eight of them,
 // six warps a row of 1536, ran at 3.3 TB/s, an instruction issued in 68% of cycles.
 //
